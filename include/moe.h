@@ -54,6 +54,13 @@ extern "C" {
 #define MOE_MAX_D      8192   /* d_model upper bound of the GEMV kernels */
 #define MOE_MAX_TOKENS    8   /* tokens per call of moe_expert_ffn_tokens */
 #define MOE_TOKENS_LDS_BYTES 131072   /* moe_expert_ffn_tokens: T * d * 4 bytes at most */
+#define MOE_LAYER_MAX_TOKENS 16       /* tokens per call of moe_layer_tokens */
+#define MOE_LAYER_MAX_VALUES 32768    /* moe_layer_tokens: T * d at most */
+#define MOE_LAYER_MAX_F (1 << 20)     /* moe_layer_tokens: f and f_shared upper bound */
+
+/* Type of activations (x, y_in and y) of the functions that take one. */
+#define MOE_F32  0
+#define MOE_BF16 1
 
 /* Message of the last failing call on the calling thread ("" if none). */
 const char *moe_last_error(void);
@@ -228,6 +235,41 @@ size_t moe_ffn_tokens_workspace_bytes(int T, int k, int d, int f);
 int moe_expert_ffn_tokens(const float *x, const void *slot_pool, int n_slots, const int32_t *slots,
                           const float *w, int T, int k, int d, int f, float *y,
                           void *workspace, size_t workspace_bytes, void *stream);
+
+/* ------------------------------------------------------------------------- */
+/* A whole MoE layer for a few tokens, routed on the device.                  */
+/* ------------------------------------------------------------------------- */
+typedef struct moe_tokens_desc {
+    int d, f;                /* d_model, d_ffn of a routed expert */
+    int n, k;                /* experts, experts per token */
+    int f_shared;            /* d_ffn of an always-active shared expert, 0 = none */
+    int n_slots;             /* slabs in slot_pool */
+    const float *w_router;   /* device fp32 [n][d] */
+    const void *slot_pool;   /* device, n_slots slabs of moe_slab_bytes(d, f) (NULL if n_slots == 0) */
+    const int32_t *slotmap;  /* device int32 [n], the slot of each expert; NULL: expert e is in slot e */
+    const void *shared;      /* device, the shared expert's slab (d, f_shared), or NULL */
+} moe_tokens_desc;
+/*
+ * One layer for the T tokens of a decode batch (several requests, speculative tokens):
+ *   y[t] = y_in[t] + sum_{e selected by t} g[t][e] FFN_e(x[t]) + FFN_shared(x[t])
+ * with the router of moe_router_topk. The routing stays on the device, so the call can be
+ * captured into a graph; each selected expert's slab is read once for all the tokens that
+ * selected it, and the shared expert's once. An expert whose slot is outside [0, n_slots)
+ * contributes nothing (its share is the caller's, who finds it in idx and w; a negative slot is
+ * the table's "not cached").
+ * x, y_in, y   device [T][d] of act_type (MOE_F32 or MOE_BF16); y_in may be NULL (zero) or y
+ *              itself. fp32 activations enter the products exactly (three bf16 parts), hidden
+ *              values of a bf16 layer as two bf16 parts; sums are fp32, a bf16 y is rounded once.
+ * idx, w       device int32 / fp32 [T][k], the routing as moe_router_topk gives it; may be NULL
+ * workspace    device, 256-byte aligned, >= moe_layer_tokens_workspace_bytes(T, d, f, n, k,
+ *              f_shared); its content before the call does not matter. Calls that may run at
+ *              the same time need workspaces of their own.
+ * 0 <= T <= MOE_LAYER_MAX_TOKENS (T == 0 is a no-op), T*d <= MOE_LAYER_MAX_VALUES, d <= MOE_MAX_D,
+ * f, f_shared <= MOE_LAYER_MAX_F, all multiples of 8; MOE_EINVAL otherwise.
+ */
+size_t moe_layer_tokens_workspace_bytes(int T, int d, int f, int n, int k, int f_shared);
+int moe_layer_tokens(const moe_tokens_desc *P, const void *x, int T, const void *y_in, void *y, int32_t *idx, float *w,
+                     int act_type, void *workspace, size_t workspace_bytes, void *stream);
 
 /* ------------------------------------------------------------------------- */
 /* Weighted combine (Section I layer output; Section III-A hit/miss split).   */

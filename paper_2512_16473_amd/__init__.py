@@ -15,7 +15,7 @@ import ctypes
 import numpy as np
 
 from . import _abi
-from ._abi import LayerDesc, PrefillDesc, RuntimeStats
+from ._abi import LayerDesc, PrefillDesc, RuntimeStats, TokensDesc
 from ._abi import MAX_D, MAX_EXPERTS, MAX_TOKENS, MAX_TOPK  # noqa: F401  (ABI bounds)
 
 _lib = _abi.load()
@@ -24,6 +24,7 @@ __all__ = [
     "MoeError", "lib", "slab_bytes", "router_topk", "Cache", "ffn_workspace_bytes", "expert_ffn_hits",
     "combine", "PinnedBuffer", "HostPool", "Runtime", "prefill_workspace_bytes", "prefill_forward", "read_stream",
     "ffn_tokens_workspace_bytes", "expert_ffn_tokens", "ffn_noalloc_max_bytes", "expert_ffn_hits_noalloc",
+    "layer_tokens_workspace_bytes", "layer_tokens",
 ]
 
 
@@ -200,6 +201,70 @@ def expert_ffn_tokens(x, slot_pool, n_slots, slots, w, d, f, y, workspace, strea
     _check("moe_expert_ffn_tokens", _lib.moe_expert_ffn_tokens(
         _ptr(x), _ptr(slot_pool), n_slots, _ptr(slots), _ptr(w), T, k, d, f, _ptr(y),
         _ptr(workspace), workspace.numel() * workspace.element_size(), _stream(stream)))
+    return y
+
+
+# --------------------------------------------------------------------------- whole layer, a few tokens
+def _act_type(t):
+    """MOE_F32 or MOE_BF16 for a tensor of activations."""
+    import torch
+    kinds = {torch.float32: _abi.F32, torch.bfloat16: _abi.BF16}
+    if t.dtype not in kinds:
+        raise ValueError(f"activations must be float32 or bfloat16, not {t.dtype}")
+    return kinds[t.dtype]
+
+
+def _want(fn, name, t, shape, dtype, device):
+    """A tensor argument as the library reads it: contiguous, of that shape and type, on x's device."""
+    if t is None:
+        return
+    if tuple(t.shape) != tuple(shape) or t.dtype != dtype or t.device != device or not t.is_contiguous():
+        raise ValueError(f"{fn}: {name} must be a contiguous {dtype} tensor of shape {tuple(shape)} on {device}, "
+                         f"not {t.dtype} {tuple(t.shape)} (strides {t.stride()}) on {t.device}")
+
+
+def _on_device(fn, x):
+    """The library launches on the current device."""
+    import torch
+    if x.device.type != "cuda":
+        raise ValueError(f"{fn}: x must be on the GPU, not on {x.device}")
+    return torch.cuda.device(x.device)
+
+
+def layer_tokens_workspace_bytes(T, d, f, n, k, f_shared=0) -> int:
+    return int(_lib.moe_layer_tokens_workspace_bytes(T, d, f, n, k, f_shared))
+
+
+def layer_tokens(x, w_router, slot_pool, f, k, y, workspace, n_slots=None, slotmap=None, shared=None, f_shared=0,
+                 y_in=None, idx=None, w=None, stream=None):
+    """y[t] = y_in[t] + the routed experts' output for x[t] (+ the shared expert's), the whole
+    layer for up to 16 tokens, routed on the device. x, y, y_in: cuda fp32 or bf16 [T, d];
+    w_router: cuda fp32 [n, d]; slot_pool: n_slots slabs (default n), expert e in slot
+    slotmap[e] (cuda int32 [n]; default e), without a valid slot contributing nothing;
+    idx int32 / w fp32 [T, k] receive the routing if given. Runs on x's device."""
+    import torch
+    T, d = x.shape
+    n = int(w_router.shape[0])
+    fn, act = "layer_tokens", _act_type(x)
+    n_slots = n if n_slots is None else int(n_slots)
+    _want(fn, "x", x, (T, d), x.dtype, x.device)
+    _want(fn, "y", y, (T, d), x.dtype, x.device)
+    _want(fn, "y_in", y_in, (T, d), x.dtype, x.device)
+    _want(fn, "w_router", w_router, (n, d), torch.float32, x.device)
+    _want(fn, "slotmap", slotmap, (n,), torch.int32, x.device)
+    _want(fn, "idx", idx, (T, k), torch.int32, x.device)
+    _want(fn, "w", w, (T, k), torch.float32, x.device)
+    for name, t, need in (("slot_pool", slot_pool, n_slots * slab_bytes(d, f)),
+                          ("shared", shared, 6 * d * f_shared)):
+        if need > 0 and (t is None or t.device != x.device or not t.is_contiguous()
+                         or t.numel() * t.element_size() < need):
+            raise ValueError(f"{fn}: {name} must hold {need} contiguous bytes on {x.device}")
+    P = TokensDesc(d, f, n, k, f_shared, n_slots, w_router.data_ptr(), None if slot_pool is None else slot_pool.data_ptr(),
+                   None if slotmap is None else slotmap.data_ptr(), None if shared is None else shared.data_ptr())
+    with _on_device(fn, x):
+        _check("moe_layer_tokens", _lib.moe_layer_tokens(
+            ctypes.byref(P), _ptr(x), T, _ptr(y_in), _ptr(y), _ptr(idx), _ptr(w), act, _ptr(workspace),
+            workspace.numel() * workspace.element_size(), _stream(stream)))
     return y
 
 

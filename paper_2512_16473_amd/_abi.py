@@ -16,6 +16,8 @@ c_char_p = ctypes.c_char_p
 
 MOE_OK, MOE_EINVAL, MOE_EHIP, MOE_ESTATE, MOE_ENOMEM = 0, -1, -2, -3, -4
 MAX_EXPERTS, MAX_TOPK, MAX_D, MAX_TOKENS = 256, 16, 8192, 8
+LAYER_MAX_TOKENS, LAYER_MAX_VALUES, LAYER_MAX_F = 16, 32768, 1 << 20
+F32, BF16 = 0, 1   # types of activations
 HOST_DOT = {"auto": 0, "fp32": 1, "bf16": 2}
 
 
@@ -43,6 +45,11 @@ class RuntimeStats(ctypes.Structure):
 class PrefillDesc(ctypes.Structure):
     _fields_ = [("d", c_int), ("f", c_int), ("n", c_int), ("k", c_int),
                 ("w_router", c_void_p), ("expert_pool", c_void_p)]
+
+
+class TokensDesc(ctypes.Structure):
+    _fields_ = [("d", c_int), ("f", c_int), ("n", c_int), ("k", c_int), ("f_shared", c_int), ("n_slots", c_int),
+                ("w_router", c_void_p), ("slot_pool", c_void_p), ("slotmap", c_void_p), ("shared", c_void_p)]
 
 
 # (name, restype, argtypes) for every function the header declares.
@@ -73,6 +80,9 @@ SIGNATURES = [
     ("moe_ffn_tokens_workspace_bytes", c_size_t, [c_int, c_int, c_int, c_int]),
     ("moe_expert_ffn_tokens", c_int, [c_void_p, c_void_p, c_int, c_void_p, c_void_p, c_int, c_int, c_int, c_int,
                                       c_void_p, c_void_p, c_size_t, c_void_p]),
+    ("moe_layer_tokens_workspace_bytes", c_size_t, [c_int] * 6),
+    ("moe_layer_tokens", c_int, [ctypes.POINTER(TokensDesc), c_void_p, c_int, c_void_p, c_void_p, c_void_p, c_void_p,
+                                 c_int, c_void_p, c_size_t, c_void_p]),
     ("moe_host_alloc", c_int, [c_size_t, ctypes.POINTER(c_void_p)]),
     ("moe_host_free", c_int, [c_void_p]),
     ("moe_host_pool_create", c_int, [c_int, ctypes.POINTER(c_void_p)]),

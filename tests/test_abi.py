@@ -425,3 +425,42 @@ def test_host_pool_dot_kinds_and_shared_use():
 def _abi_lib():
     from paper_2512_16473_amd import _lib
     return _lib
+
+
+def _layer_call(T=2, d=64, f=64, n=4, k=2, fs=0, slots=4, act=0, ws=256, nbytes=1 << 40, x=256, y=256, y_in=None, wr=256,
+                pool=256, shared=None, desc=True):
+    """moe_layer_tokens with made-up addresses: only calls that are refused before any launch."""
+    lib = moe.lib()
+    P = _abi.TokensDesc(d, f, n, k, fs, slots, wr, pool, None, shared)
+    return lib.moe_layer_tokens(ctypes.byref(P) if desc else None, x, T, y_in, y, None, None, act, ws, nbytes, None)
+
+
+@pytest.mark.parametrize("bad,message", [
+    (dict(desc=False), b"null descriptor"), (dict(act=2), b"act_type=2"), (dict(T=-1), b"T=-1"), (dict(T=17), b"T=17"),
+    (dict(d=60), b"d=60"), (dict(d=0), b"d=0"), (dict(d=8200), b"d=8200"), (dict(T=9, d=4096), b"T*d=36864"),
+    (dict(f=12), b"f=12"), (dict(f=0), b"f=0"), (dict(f=(1 << 20) + 8), b"f=1048584"), (dict(fs=4), b"f_shared=4"),
+    (dict(fs=-8), b"f_shared=-8"), (dict(n=0, k=0), b"n=0"), (dict(n=257), b"n=257"), (dict(k=5), b"k=5"),
+    (dict(k=0), b"k=0"), (dict(n=64, k=17), b"k=17"), (dict(slots=-1), b"n_slots=-1"), (dict(x=None), b"null pointer"),
+    (dict(y=None), b"null pointer"), (dict(wr=None), b"null pointer"), (dict(pool=None), b"null pointer"),
+    (dict(fs=64), b"null pointer"), (dict(ws=None), b"null pointer"), (dict(x=264), b"16-byte aligned"),
+    (dict(y=260), b"16-byte aligned"), (dict(y_in=8), b"16-byte aligned"), (dict(pool=8), b"16-byte aligned"),
+    (dict(wr=8), b"16-byte aligned"), (dict(fs=64, shared=8), b"16-byte aligned"), (dict(ws=128), b"256-byte aligned"),
+    (dict(nbytes=0), b"workspace 0 <"),
+])
+def test_layer_tokens_refusals(bad, message):
+    assert _layer_call(**bad) == _abi.MOE_EINVAL
+    assert message in moe.lib().moe_last_error()
+
+
+def test_layer_tokens_workspace_sizes():
+    """One byte less than either type needs is refused; no tokens are no call."""
+    for T, d, f, n, k, fs in ((1, 256, 512, 4, 2, 0), (16, 2048, 264, 60, 8, 136), (8, 4096, 14336, 8, 2, 0),
+                              (16, 128, 8, 256, 16, 20480), (1, 8, 8, 1, 1, 0)):
+        need = []
+        for act in (_abi.F32, _abi.BF16):
+            assert _layer_call(T=T, d=d, f=f, n=n, k=k, fs=fs, shared=256, act=act, nbytes=0) == _abi.MOE_EINVAL
+            need.append(int(re.search(rb"workspace 0 < (\d+) bytes", moe.lib().moe_last_error()).group(1)))
+        assert moe.layer_tokens_workspace_bytes(T, d, f, n, k, fs) == max(need)
+    assert _layer_call(T=0, x=None, y=None, ws=None) == _abi.MOE_OK
+    for bad in ((0, 64, 64, 4, 2, 0), (17, 64, 64, 4, 2, 0), (1, 0, 64, 4, 2, 0), (1, 64, 64, 4, 17, 0), (1, 64, 64, 4, 2, -8)):
+        assert moe.layer_tokens_workspace_bytes(*bad) == 0
