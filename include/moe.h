@@ -57,6 +57,9 @@ extern "C" {
 #define MOE_LAYER_MAX_TOKENS 16       /* tokens per call of moe_layer_tokens */
 #define MOE_LAYER_MAX_VALUES 32768    /* moe_layer_tokens: T * d at most */
 #define MOE_LAYER_MAX_F (1 << 20)     /* moe_layer_tokens: f and f_shared upper bound */
+#define MOE_ADAPTER_MAX_TOKENS 65536  /* tokens per call of moe_adapter_project */
+#define MOE_ADAPTER_MAX_RANK 128
+#define MOE_ADAPTER_MAX_D (1 << 20)   /* moe_adapter_project: d_in and d_out upper bound */
 
 /* Type of activations (x, y_in and y) of the functions that take one. */
 #define MOE_F32  0
@@ -270,6 +273,38 @@ typedef struct moe_tokens_desc {
 size_t moe_layer_tokens_workspace_bytes(int T, int d, int f, int n, int k, int f_shared);
 int moe_layer_tokens(const moe_tokens_desc *P, const void *x, int T, const void *y_in, void *y, int32_t *idx, float *w,
                      int act_type, void *workspace, size_t workspace_bytes, void *stream);
+
+/* ------------------------------------------------------------------------- */
+/* Low-rank adapters of many requests beside a projection they share.         */
+/* ------------------------------------------------------------------------- */
+typedef struct moe_adapter_desc {
+    int d_in, d_out;
+    int n_adapters, rank;    /* adapters held, their rank (smaller ones padded with zeros) */
+    const void *w;           /* device bf16 [d_out][d_in], e.g. W1, W3 or W2 of a slab; NULL: the adapters alone */
+    const void *a;           /* device bf16 [n_adapters][rank][d_in] */
+    const void *b;           /* device bf16 [n_adapters][d_out][rank] */
+    const float *scale;      /* device fp32 [n_adapters], NULL: 1 */
+} moe_adapter_desc;
+/*
+ *   y[t] = y_in[t] + W x[t] + scale[i] B_i (A_i x[t]),  i = adapters[t]
+ * for T tokens of different requests: W is read once for all of them, each adapter once per
+ * block of tokens that uses it. A token whose adapters[t] is outside [0, n_adapters) has none.
+ * Any order of tokens is right; those of one adapter side by side are fastest.
+ * x, y_in, y   device, rows of d_in / d_out values of act_type (MOE_F32 or MOE_BF16), row strides
+ *              in elements (multiples of 8); y_in may be NULL (zero) or y itself. fp32 activations
+ *              enter the products exactly (three bf16 parts, so beyond 16 tokens an fp32 call does
+ *              three times a bf16 call's matrix work); sums are fp32, a bf16 y is rounded once.
+ * adapters     device int32 [T]
+ * workspace    device, 256-byte aligned, >= moe_adapter_workspace_bytes(T, d_in, d_out, rank,
+ *              act_type); its content before the call does not matter. Calls that may run at the
+ *              same time need workspaces of their own.
+ * 0 <= T <= MOE_ADAPTER_MAX_TOKENS (T == 0 is a no-op), d_in, d_out <= MOE_ADAPTER_MAX_D, rank <=
+ * MOE_ADAPTER_MAX_RANK, all three multiples of 8; MOE_EINVAL otherwise.
+ */
+size_t moe_adapter_workspace_bytes(int T, int d_in, int d_out, int rank, int act_type);
+int moe_adapter_project(const moe_adapter_desc *P, const void *x, int64_t x_stride, int T, const int32_t *adapters,
+                        const void *y_in, int64_t y_in_stride, void *y, int64_t y_stride, int act_type, void *workspace,
+                        size_t workspace_bytes, void *stream);
 
 /* ------------------------------------------------------------------------- */
 /* Weighted combine (Section I layer output; Section III-A hit/miss split).   */

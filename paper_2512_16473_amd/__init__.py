@@ -15,7 +15,7 @@ import ctypes
 import numpy as np
 
 from . import _abi
-from ._abi import LayerDesc, PrefillDesc, RuntimeStats, TokensDesc
+from ._abi import AdapterDesc, LayerDesc, PrefillDesc, RuntimeStats, TokensDesc
 from ._abi import MAX_D, MAX_EXPERTS, MAX_TOKENS, MAX_TOPK  # noqa: F401  (ABI bounds)
 
 _lib = _abi.load()
@@ -24,7 +24,7 @@ __all__ = [
     "MoeError", "lib", "slab_bytes", "router_topk", "Cache", "ffn_workspace_bytes", "expert_ffn_hits",
     "combine", "PinnedBuffer", "HostPool", "Runtime", "prefill_workspace_bytes", "prefill_forward", "read_stream",
     "ffn_tokens_workspace_bytes", "expert_ffn_tokens", "ffn_noalloc_max_bytes", "expert_ffn_hits_noalloc",
-    "layer_tokens_workspace_bytes", "layer_tokens",
+    "layer_tokens_workspace_bytes", "layer_tokens", "adapter_workspace_bytes", "adapter_project",
 ]
 
 
@@ -264,6 +264,55 @@ def layer_tokens(x, w_router, slot_pool, f, k, y, workspace, n_slots=None, slotm
     with _on_device(fn, x):
         _check("moe_layer_tokens", _lib.moe_layer_tokens(
             ctypes.byref(P), _ptr(x), T, _ptr(y_in), _ptr(y), _ptr(idx), _ptr(w), act, _ptr(workspace),
+            workspace.numel() * workspace.element_size(), _stream(stream)))
+    return y
+
+
+# --------------------------------------------------------------------------- adapters beside a projection
+def _want_rows(fn, name, t, shape, dtype, device):
+    """Rows of contiguous values, any row stride."""
+    if t is None:
+        return
+    if tuple(t.shape) != tuple(shape) or t.dtype != dtype or t.device != device or t.stride(1) != 1:
+        raise ValueError(f"{fn}: {name} must be a {dtype} tensor of shape {tuple(shape)} on {device} with contiguous rows, "
+                         f"not {t.dtype} {tuple(t.shape)} (strides {t.stride()}) on {t.device}")
+
+
+def _row_stride(t):
+    """Elements from row to row (one row alone has any)."""
+    return t.stride(0) if t.shape[0] > 1 else t.shape[1]
+
+
+def adapter_workspace_bytes(T, d_in, d_out, rank, dtype) -> int:
+    import torch
+    act = {torch.float32: _abi.F32, torch.bfloat16: _abi.BF16}.get(dtype, -1)
+    return int(_lib.moe_adapter_workspace_bytes(T, d_in, d_out, rank, act))
+
+
+def adapter_project(x, w, a, b, adapters, y, workspace, scale=None, y_in=None, stream=None):
+    """y[t] = y_in[t] + w x[t] + scale[i] b[i] (a[i] x[t]) with i = adapters[t], the low-rank
+    adapter of token t's request (none outside [0, n)). x [T, d_in], y and y_in [T, d_out]: cuda
+    fp32 or bf16, rows contiguous; w: cuda bf16 [d_out, d_in] or None; a: bf16 [n, rank, d_in];
+    b: bf16 [n, d_out, rank]; adapters: int32 [T]; scale: fp32 [n]. Runs on x's device."""
+    import torch
+    fn, act = "adapter_project", _act_type(x)
+    T, d_in = x.shape
+    n, rank = int(a.shape[0]), int(a.shape[1])
+    d_out = int(b.shape[1])
+    _want_rows(fn, "x", x, (T, d_in), x.dtype, x.device)
+    _want_rows(fn, "y", y, (T, d_out), x.dtype, x.device)
+    _want_rows(fn, "y_in", y_in, (T, d_out), x.dtype, x.device)
+    _want(fn, "w", w, (d_out, d_in), torch.bfloat16, x.device)
+    _want(fn, "a", a, (n, rank, d_in), torch.bfloat16, x.device)
+    _want(fn, "b", b, (n, d_out, rank), torch.bfloat16, x.device)
+    _want(fn, "adapters", adapters, (T,), torch.int32, x.device)
+    _want(fn, "scale", scale, (n,), torch.float32, x.device)
+    P = AdapterDesc(d_in, d_out, n, rank, None if w is None else w.data_ptr(), a.data_ptr(), b.data_ptr(),
+                    None if scale is None else scale.data_ptr())
+    with _on_device(fn, x):
+        _check("moe_adapter_project", _lib.moe_adapter_project(
+            ctypes.byref(P), _ptr(x), _row_stride(x), T, _ptr(adapters), _ptr(y_in),
+            0 if y_in is None else _row_stride(y_in), _ptr(y), _row_stride(y), act, _ptr(workspace),
             workspace.numel() * workspace.element_size(), _stream(stream)))
     return y
 

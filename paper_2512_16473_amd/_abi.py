@@ -9,6 +9,7 @@ LIB_PATH = os.path.join(_HERE, "libmoe.so")
 
 c_int, c_size_t, c_void_p, c_float, c_double = (ctypes.c_int, ctypes.c_size_t, ctypes.c_void_p,
                                                 ctypes.c_float, ctypes.c_double)
+c_int64 = ctypes.c_int64
 c_i32p = ctypes.POINTER(ctypes.c_int32)
 c_u8p = ctypes.POINTER(ctypes.c_uint8)
 c_f32p = ctypes.POINTER(ctypes.c_float)
@@ -17,6 +18,7 @@ c_char_p = ctypes.c_char_p
 MOE_OK, MOE_EINVAL, MOE_EHIP, MOE_ESTATE, MOE_ENOMEM = 0, -1, -2, -3, -4
 MAX_EXPERTS, MAX_TOPK, MAX_D, MAX_TOKENS = 256, 16, 8192, 8
 LAYER_MAX_TOKENS, LAYER_MAX_VALUES, LAYER_MAX_F = 16, 32768, 1 << 20
+ADAPTER_MAX_TOKENS, ADAPTER_MAX_RANK, ADAPTER_MAX_D = 65536, 128, 1 << 20
 F32, BF16 = 0, 1   # types of activations
 HOST_DOT = {"auto": 0, "fp32": 1, "bf16": 2}
 
@@ -52,6 +54,11 @@ class TokensDesc(ctypes.Structure):
                 ("w_router", c_void_p), ("slot_pool", c_void_p), ("slotmap", c_void_p), ("shared", c_void_p)]
 
 
+class AdapterDesc(ctypes.Structure):
+    _fields_ = [("d_in", c_int), ("d_out", c_int), ("n_adapters", c_int), ("rank", c_int),
+                ("w", c_void_p), ("a", c_void_p), ("b", c_void_p), ("scale", c_void_p)]
+
+
 # (name, restype, argtypes) for every function the header declares.
 SIGNATURES = [
     ("moe_last_error", c_char_p, []),
@@ -83,6 +90,9 @@ SIGNATURES = [
     ("moe_layer_tokens_workspace_bytes", c_size_t, [c_int] * 6),
     ("moe_layer_tokens", c_int, [ctypes.POINTER(TokensDesc), c_void_p, c_int, c_void_p, c_void_p, c_void_p, c_void_p,
                                  c_int, c_void_p, c_size_t, c_void_p]),
+    ("moe_adapter_workspace_bytes", c_size_t, [c_int] * 5),
+    ("moe_adapter_project", c_int, [ctypes.POINTER(AdapterDesc), c_void_p, c_int64, c_int, c_void_p, c_void_p, c_int64,
+                                    c_void_p, c_int64, c_int, c_void_p, c_size_t, c_void_p]),
     ("moe_host_alloc", c_int, [c_size_t, ctypes.POINTER(c_void_p)]),
     ("moe_host_free", c_int, [c_void_p]),
     ("moe_host_pool_create", c_int, [c_int, ctypes.POINTER(c_void_p)]),

@@ -464,3 +464,40 @@ def test_layer_tokens_workspace_sizes():
     assert _layer_call(T=0, x=None, y=None, ws=None) == _abi.MOE_OK
     for bad in ((0, 64, 64, 4, 2, 0), (17, 64, 64, 4, 2, 0), (1, 0, 64, 4, 2, 0), (1, 64, 64, 4, 17, 0), (1, 64, 64, 4, 2, -8)):
         assert moe.layer_tokens_workspace_bytes(*bad) == 0
+
+
+def _adapter_call(T=2, d=64, o=64, n=4, r=8, act=0, ws=256, nbytes=1 << 40, x=256, y=256, y_in=None, w=256, a=256, b=256,
+                  ids=256, xs=64, ys=64, yis=64, desc=True):
+    """moe_adapter_project with made-up addresses: only calls that are refused before any launch."""
+    P = _abi.AdapterDesc(d, o, n, r, w, a, b, None)
+    return moe.lib().moe_adapter_project(ctypes.byref(P) if desc else None, x, xs, T, ids, y_in, yis, y, ys, act, ws, nbytes,
+                                         None)
+
+
+@pytest.mark.parametrize("bad,message", [
+    (dict(desc=False), b"null descriptor"), (dict(act=-1), b"act_type=-1"), (dict(T=-1), b"T=-1"), (dict(T=65537), b"T=65537"),
+    (dict(d=60), b"d_in=60"), (dict(d=0), b"d_in=0"), (dict(d=(1 << 20) + 8), b"d_in=1048584"), (dict(o=4), b"d_out=4"),
+    (dict(o=0), b"d_out=0"), (dict(o=(1 << 20) + 8), b"d_out=1048584"), (dict(n=-1), b"n_adapters=-1"), (dict(r=0), b"rank=0"),
+    (dict(r=12), b"rank=12"), (dict(r=136), b"rank=136"), (dict(x=None), b"null pointer"), (dict(y=None), b"null pointer"),
+    (dict(ids=None), b"null pointer"), (dict(a=None), b"null pointer"), (dict(b=None), b"null pointer"),
+    (dict(ws=None), b"null pointer"), (dict(xs=56), b"x_stride=56"), (dict(xs=68), b"x_stride=68"), (dict(ys=60), b"y_stride=60"),
+    (dict(y_in=512, yis=32), b"y_in_stride=32"), (dict(y_in=256, yis=72), b"another stride"), (dict(x=264), b"16-byte aligned"),
+    (dict(y=264), b"16-byte aligned"), (dict(w=8), b"16-byte aligned"), (dict(a=8), b"16-byte aligned"),
+    (dict(b=8), b"16-byte aligned"), (dict(ws=128), b"256-byte aligned"), (dict(nbytes=0), b"workspace 0 <"),
+])
+def test_adapter_refusals(bad, message):
+    assert _adapter_call(**bad) == _abi.MOE_EINVAL
+    assert message in moe.lib().moe_last_error()
+
+
+def test_adapter_workspace_sizes():
+    import torch
+    for T, d, o, r in ((1, 8, 8, 8), (16, 14336, 4096, 128), (17, 264, 520, 24), (4096, 4096, 14336, 64)):
+        for act, dtype in ((_abi.F32, torch.float32), (_abi.BF16, torch.bfloat16)):
+            assert _adapter_call(T=T, d=d, o=o, r=r, act=act, xs=d, ys=o, nbytes=0) == _abi.MOE_EINVAL
+            need = int(re.search(rb"workspace 0 < (\d+) bytes", moe.lib().moe_last_error()).group(1))
+            assert moe.adapter_workspace_bytes(T, d, o, r, dtype) == need
+    assert _adapter_call(T=0, x=None, y=None, ws=None, ids=None) == _abi.MOE_OK
+    for bad in ((0, 64, 64, 8, 0), (65537, 64, 64, 8, 0), (1, 0, 64, 8, 0), (1, 64, 64, 136, 0), (1, 64, 64, 8, 2)):
+        assert moe.lib().moe_adapter_workspace_bytes(*bad) == 0
+    assert moe.adapter_workspace_bytes(1, 64, 64, 8, torch.float16) == 0
