@@ -3,20 +3,22 @@
 //
 // Up to 16 tokens (a decode batch) W is streamed once past all of them (row_stream.h); longer
 // batches are a tiled matrix product. Kernels, on one stream:
-//   1. shrink: v_t = A_a x_t. Per block of tokens the adapters among them, each a few blocks of
-//      16 rows, are multiplied with all the block's tokens; a token keeps its own adapter's sums.
 //   up to 16 tokens:
+//   1. prepare: v_t = scale_a A_a x_t, a few waves per (token, rank); and x as operand columns;
 //   2. rows: blocks of 16 rows of W against all the tokens, the columns cut into groups of up
-//      to 8 units as in the layer's down projection; with one group the expansion B_a v_t, y_in
-//      and the rounding follow in the same kernel, else
-//   3. finish adds the groups in order, the expansion and y_in.
+//      to 8 units as in the layer's down projection. The adapters in the batch are shared out
+//      among a work group's waves: after its chunks of W a wave streams the 16 rows of its
+//      adapters' B and multiplies them with all the v; a token takes its own adapter's.
 //   longer:
-//   2. parts: v scaled and cut into bf16 parts; the activations too where they are fp32 or their
-//      rows do not end with a K step; and the list of adapters in every tile of tokens;
-//   3. gemm: tiles of up to 256 tokens by 256 rows of W; after the K steps of W, each adapter
-//      in the tile adds a few more: its B rows against the tile's v, rows of other adapters
-//      zero. The tiles of a last, partial round of work groups are split over K, and
-//   4. tail adds their parts.
+//   1. cast: the activations as bf16 parts, where they are fp32 or their rows do not end with a K
+//      step;
+//   2. shrink: v, per block of tokens: the adapters among them, each a few blocks of 16 rows of
+//      A, are multiplied with all the block's tokens; a token keeps its own adapter's sums;
+//   3. parts: v scaled and cut into bf16 parts, and the adapters in every tile of tokens;
+//   4. gemm: tiles of up to 256 tokens by 256 rows of W; after the K steps of W, each adapter
+//      in the tile adds a few more: its B rows against the tile's v, the products kept by its own
+//      tokens. The tiles of a last, partial round of work groups are split over K, and
+//   5. tail adds their parts.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -34,7 +36,7 @@ namespace {
 using namespace row_stream;
 
 constexpr int kStreamTokens = 16;    // tokens that the rows kernel takes
-constexpr int kBlockTokens = 64;     // tokens per shrink block, at most
+constexpr int kBlockTokens = 64;     // tokens per shrink block of a longer one, at most
 
 struct AdapterParams {
     const void *x;                // [T][ldx]
@@ -45,17 +47,28 @@ struct AdapterParams {
     const int32_t *ids;           // [T]
     const float *scale;           // [n] or null
     int T, d, o, n, r;
-    int tb;                       // tokens per shrink block
-    int vgroups;                  // K groups of v
-    float *v;                     // [vgroups][T][r]
-    float *partial;               // [groups][T][o]
-    int groups;
     const void *y_in;             // or null
     void *y;
+    // up to 16 tokens
+    uint8_t *xc;                  // x as columns (row_stream.h)
+    uint16_t *vc;                 // [parts][T][rank chunks * kChunk] v in bf16 parts
+    float *partial;               // [groups][T][o]
+    uint32_t *counts;             // [row blocks of y]
+    int groups;
+    // longer
+    int tb;                       // tokens per shrink block
+    int vgroups;                  // K groups of v
+    float *v;                     // [vgroups][T][r], unscaled
+    const uint16_t *xk;           // activations in bf16, their parts side by side: [T][ldk], a part kpart values
+    int64_t ldk, kpart;
 };
 
 __device__ __forceinline__ bool has_adapter(const AdapterParams &p, int id) { return id >= 0 && id < p.n; }
 __device__ __forceinline__ float scale_of(const AdapterParams &p, int id) { return p.scale ? p.scale[id] : 1.f; }
+__host__ __device__ inline int x_parts(bool bf16) { return bf16 ? 1 : 3; }
+// v meets B in three exact parts; beside bf16 activations in two (2^-17 relative)
+__host__ __device__ inline int v_parts(bool bf16) { return bf16 ? 2 : 3; }
+__device__ __forceinline__ uint16_t v_part(bool bf16, float v, int q) { return bf16 ? part_of<2>(v, q) : part_of<3>(v, q); }
 __device__ __forceinline__ float load_act(const void *x, bool bf16, size_t at)
 {
     return bf16 ? static_cast<float>(static_cast<const __bf16 *>(x)[at]) : static_cast<const float *>(x)[at];
@@ -65,70 +78,151 @@ __device__ __forceinline__ void store_act(void *y, bool bf16, size_t at, float v
     if (bf16) static_cast<__bf16 *>(y)[at] = static_cast<__bf16>(v);
     else static_cast<float *>(y)[at] = v;
 }
-
-// The B operand's fragments of this wave's chunks [c0, c0 + cnt): tokens t0 .. of tn, fp32 ones
-// as three columns each (part by part).
-template <int S, int NB>
-__device__ __forceinline__ void load_tokens(const AdapterParams &p, int t0, int tn, int c0, int cnt, bf16x8_t (&bx)[S][2][NB])
+// 8 activations' parts q, as bf16.
+__device__ __forceinline__ uint4 act_part(const AdapterParams &p, size_t at, int q)
 {
-    const int lane = threadIdx.x & 63, parts = p.bf16 ? 1 : 3;
+    if (p.bf16) return *reinterpret_cast<const uint4 *>(static_cast<const uint16_t *>(p.x) + at);
+    const float4 *src = reinterpret_cast<const float4 *>(static_cast<const float *>(p.x) + at);
+    const float4 a = src[0], b = src[1];
+    const float f[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+    uint32_t u[4];
 #pragma unroll
-    for (int nb = 0; nb < NB; ++nb) {
-        const int c = nb * 16 + (lane & 15), part = c / tn, t = c - part * tn;
-#pragma unroll
-        for (int s = 0; s < S; ++s)
-#pragma unroll
-            for (int kb = 0; kb < 2; ++kb) {
-                const int k = (c0 + s) * kChunk + kb * 32 + (lane >> 4) * 8;
-                bx[s][kb][nb] = s < cnt && k < p.d && part < parts ? load_part(p.x, p.bf16, (size_t)(t0 + t) * p.ldx + k, part)
-                                                                   : no_tokens();
+    for (int i = 0; i < 4; ++i) u[i] = part_of<3>(f[2 * i], q) | ((uint32_t)part_of<3>(f[2 * i + 1], q) << 16);
+    return make_uint4(u[0], u[1], u[2], u[3]);
+}
+
+// ------------------------------------------------------------------ up to 16 tokens
+// Blocks of the first `v_blocks`: v. A wave sums a `split`-th of a (token, rank) row of A, in fp32; the
+// work group adds up. Ranks run to whole chunks, with zeros. The other blocks: x as columns, 8 values
+// of a token and part per thread; and the row counts cleared.
+__global__ __launch_bounds__(256) void k_adapter_prepare(AdapterParams p, int split, int v_blocks)
+{
+    __shared__ float part[4];
+    if ((int)blockIdx.x >= v_blocks) {
+        const int i = (blockIdx.x - v_blocks) * 256 + threadIdx.x;
+        const int cols = p.T * x_parts(p.bf16);
+        for (int64_t j = i; j < (p.o + kRows - 1) / kRows; j += (int64_t)(gridDim.x - v_blocks) * 256) p.counts[j] = 0;
+        if (i >= chunks_of(p.d) * (kChunk / 8) * cols) return;
+        const int c = i % cols, k = i / cols * 8, q = c / p.T, t = c - q * p.T;
+        const uint4 v = k < p.d ? act_part(p, (size_t)t * p.ldx + k, q) : make_uint4(0, 0, 0, 0);
+        *reinterpret_cast<uint4 *>(p.xc + (size_t)i * 16) = v;
+        return;
+    }
+    const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6, rp = chunks_of(p.r) * kChunk;
+    const int i = blockIdx.x * (4 / split) + wv / split, t = i / rp, j = i - t * rp;
+    const int id = t < p.T ? p.ids[t] : -1;
+    const bool live = has_adapter(p, id) && j < p.r;
+    float acc = 0.f;
+    if (live) {
+        const uint4 *a = reinterpret_cast<const uint4 *>(p.a + ((size_t)id * p.r + j) * p.d * 2);
+        const int nc = p.d >> 3;
+        auto dot = [&](const uint4 w, const float4 u, const float4 v) {
+            acc = fmaf(__uint_as_float(w.x << 16), u.x, acc);
+            acc = fmaf(__uint_as_float(w.x & 0xffff0000u), u.y, acc);
+            acc = fmaf(__uint_as_float(w.y << 16), u.z, acc);
+            acc = fmaf(__uint_as_float(w.y & 0xffff0000u), u.w, acc);
+            acc = fmaf(__uint_as_float(w.z << 16), v.x, acc);
+            acc = fmaf(__uint_as_float(w.z & 0xffff0000u), v.y, acc);
+            acc = fmaf(__uint_as_float(w.w << 16), v.z, acc);
+            acc = fmaf(__uint_as_float(w.w & 0xffff0000u), v.w, acc);
+        };
+        if (p.bf16) {
+            const uint4 *x = reinterpret_cast<const uint4 *>(static_cast<const uint16_t *>(p.x) + (size_t)t * p.ldx);
+#pragma unroll 4
+            for (int c = (wv % split) * kWave + lane; c < nc; c += split * kWave) {
+                const uint4 v = x[c];
+                dot(a[c], make_float4(__uint_as_float(v.x << 16), __uint_as_float(v.x & 0xffff0000u), __uint_as_float(v.y << 16), __uint_as_float(v.y & 0xffff0000u)),
+                    make_float4(__uint_as_float(v.z << 16), __uint_as_float(v.z & 0xffff0000u), __uint_as_float(v.w << 16), __uint_as_float(v.w & 0xffff0000u)));
             }
+        } else {
+            const float4 *x = reinterpret_cast<const float4 *>(static_cast<const float *>(p.x) + (size_t)t * p.ldx);
+#pragma unroll 4
+            for (int c = (wv % split) * kWave + lane; c < nc; c += split * kWave) dot(a[c], x[2 * c], x[2 * c + 1]);
+        }
+    }
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) acc += __shfl_xor(acc, o, kWave);
+    if (lane == 0) part[wv] = acc;
+    __syncthreads();
+    if (lane == 0 && wv % split == 0 && t < p.T) {
+        for (int k = 1; k < split; ++k) acc += part[wv + k];
+        const float v = live ? acc * scale_of(p, id) : 0.f;
+        for (int q = 0; q < v_parts(p.bf16); ++q) p.vc[((size_t)q * p.T + t) * rp + j] = v_part(p.bf16, v, q);
     }
 }
 
-// Wave's chunks of group g: eight units of up to S chunks of the d columns.
-template <int S>
-__device__ __forceinline__ void group_chunks(int d, int g, int wv, int &c0, int &cnt)
+// Chunks of unit u of `units`: the whole of C in equal parts.
+__device__ __forceinline__ void unit_chunks(int C, int u, int units, int &c0, int &cnt)
 {
-    const int C = (d + kChunk - 1) / kChunk, units = (C + S - 1) / S, u = g * kWaves + wv;
     c0 = cnt = 0;
     if (u < units) part_chunks(C, u, units, c0, cnt);
 }
 
-struct ShrinkSrc {
-    const uint8_t *base0, *base1;
-    size_t half;
-    int c0, cnt;
+// A wave's item: its chunks of 16 rows of W, then the rows of its adapters' B, rank chunk by chunk.
+template <int S>
+struct RowsAndB {
+    Rows w;
+    const uint8_t *b0, *b1;   // B rows of its first and second adapter, or null
+    size_t bhalf;
+    int bbytes, blane, rc;    // bytes of a row of B, offset of this lane's, rank chunks
+};
+template <int S>
+__device__ __forceinline__ Place place_of(const RowsAndB<S> &r, int s, const uint8_t *hot)
+{
+    if (s < S) return place_of(r.w, s, hot);
+    const int e = s - S, second = e >= r.rc ? 1 : 0, q = e - second * r.rc;
+    const uint8_t *b = e >= 2 * r.rc ? nullptr : second ? r.b1 : r.b0;
+    return {b ? b : hot, b ? b + r.bhalf : hot, b ? (uint32_t)(r.blane + min(q * (kChunk * 2) + lane_piece(), r.bbytes - 16)) : 0u};
+}
+
+template <int S>
+struct RowsSrc {
     const AdapterParams &p;
-    const int *list;
-    int it, step, total, rbs;
-    template <class R>
-    __device__ __forceinline__ bool next(R &)
+    const int *list;          // distinct adapters of the batch
+    int wv, it, end, rbs, units;
+    int nlist;
+    RowsAndB<S> r;
+    __device__ __forceinline__ RowsAndB<S> next()
     {
-        if (it >= total || cnt == 0) return false;
-        const int j = it / rbs, rb = it - j * rbs;
-        const size_t K2 = (size_t)p.d * 2;
-        base0 = p.a + ((size_t)list[j] * p.r + (size_t)rb * kRows) * K2;
-        half = rb * kRows + 8 < p.r ? 8 * K2 : 0;   // the last block may have 8 rows
-        it += step;
-        return true;
+        r.w.cnt = 0;
+        r.b0 = r.b1 = nullptr;
+        if (it >= end) return r;
+        const int g = it / rbs, rb = it - g * rbs;
+        const bool whole = rb * kRows + 8 < p.o;   // the last block may have 8 rows
+        unit_chunks(chunks_of(p.d), g * kWaves + wv, units, r.w.c0, r.w.cnt);
+        r.w.base = p.w + (size_t)rb * kRows * r.w.bytes;
+        r.w.half = whole ? (size_t)8 * r.w.bytes : 0;
+        r.bhalf = whole ? (size_t)8 * r.bbytes : 0;
+        if (g == 0) {
+            if (wv < nlist) r.b0 = p.b + ((size_t)list[wv] * p.o + (size_t)rb * kRows) * r.bbytes;
+            if (wv + kWaves < nlist) r.b1 = p.b + ((size_t)list[wv + kWaves] * p.o + (size_t)rb * kRows) * r.bbytes;
+        }
+        ++it;
+        return r;
     }
 };
 
-// v of the tokens of block x, K group y; of the block's (adapter, 16 rows) items every gridDim.z-th.
-template <int S, int NB>
-__global__ __launch_bounds__(kThreads) void k_adapter_shrink(AdapterParams p)
+constexpr int kKeptSums = 4096;   // 16 KiB: 8 tokens of 32 items
+
+// W x and B v for up to 16 tokens. A work group takes an equal, contiguous share of the (group, 16
+// rows) items; the adapters' part belongs to group 0. E: stages of B per item.
+template <int S, int E, int NB>
+__global__ __launch_bounds__(kThreads) void k_adapter_rows(AdapterParams p)
 {
-    constexpr int RS = NB <= 2 ? 8 : 6;
-    constexpr int kRing = kWaves * RS * kStageBytes;
-    __shared__ __align__(1024) uint8_t lds[kRing + kWaves * NB * 1024];
-    __shared__ int list[kBlockTokens], mine[kBlockTokens], njobs;
-    const int tid = threadIdx.x, wv = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int t0 = blockIdx.x * p.tb, tn = min(p.tb, p.T - t0), g = blockIdx.y;
+    constexpr bool STK = NB == 3;
+    constexpr int AB = STK ? 1 : NB;
+    constexpr int kRankPitch = MOE_ADAPTER_MAX_RANK + 8;   // values; the pad spreads the tokens over the banks
+    using Stream_t = Stream<S + E, RowsSrc<S>, RowsAndB<S>>;
+    __shared__ __align__(1024) uint8_t lds[kWaves * Stream_t::kBytes];
+    __shared__ __align__(16) Sums<AB> sums;
+    __shared__ __align__(16) uint16_t v[3 * kStreamTokens * kRankPitch];
+    __shared__ int list[kStreamTokens], nlist, todo[kThreads];
+    __shared__ float kept[kKeptSums];
+    const int tid = threadIdx.x, lane = tid & 63, wv = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int rc = chunks_of(p.r), rp = rc * kChunk, vp = v_parts(p.bf16);
+    const int own = (lane & 15) < p.T ? p.ids[lane & 15] : -1;   // adapter of this lane's column
     if (tid < kWave) {   // the distinct adapters, in order of first appearance
-        int id = tid < tn ? p.ids[t0 + tid] : -1;
-        if (!has_adapter(p, id)) id = -1;
-        mine[tid] = id;
+        const int id = tid < p.T && has_adapter(p, own) ? own : -1;
         uint64_t m = __ballot(id >= 0);
         int n = 0;
         while (m) {
@@ -137,168 +231,81 @@ __global__ __launch_bounds__(kThreads) void k_adapter_shrink(AdapterParams p)
             ++n;
             m &= ~__ballot(id == a);
         }
-        if (tid == 0) njobs = n;
+        if (tid == 0) nlist = n;
     }
-    __syncthreads();
-    const int rbs = (p.r + kRows - 1) / kRows, total = __builtin_amdgcn_readfirstlane(njobs) * rbs;
-    if ((int)blockIdx.z >= total) return;
-    ShrinkSrc src{nullptr, nullptr, 0, 0, 0, p, list, (int)blockIdx.z, (int)gridDim.z, total, rbs};
-    group_chunks<S>(p.d, g, wv, src.c0, src.cnt);
-    Stream<S, 1, NB, RS, ShrinkSrc> st;
-    st.ring.row_bytes((int64_t)p.d * 2);
-    st.start(src, lds + wv * RS * kStageBytes);
-    bf16x8_t bx[S][2][NB];
-    load_tokens<S, NB>(p, t0, tn, src.c0, src.cnt, bx);
-    float *red = reinterpret_cast<float *>(lds + kRing);
-    const int parts = p.bf16 ? 1 : 3;
-    for (int it = blockIdx.z; it < total; it += gridDim.z) {
-        floatx4_t acc[1][NB];
-        st.item(src, bx, src.cnt, acc);
-        lds_barrier();
-        put_sums(red, wv, acc);
-        lds_barrier();
-        const int j = it / rbs, row = tid & 15, i = (it - j * rbs) * kRows + row;
-        for (int t = tid >> 4; t < tn; t += kThreads / kRows) {
-            if (i >= p.r || mine[t] != list[j]) continue;
-            float v = 0.f;
-            for (int q = 0; q < parts; ++q) v += get_sum<1, NB>(red, 0, row, q * tn + t);
-            p.v[((size_t)g * p.T + t0 + t) * p.r + i] = v;
-        }
+    for (int i = tid; i < vp * p.T * rp / 8; i += kThreads) {
+        const int q = i * 8 / rp, k = i * 8 - q * rp;   // q: part * T + token
+        const int part = q / p.T, t = q - part * p.T;
+        *reinterpret_cast<uint4 *>(&v[(part * kStreamTokens + t) * kRankPitch + k]) = *reinterpret_cast<const uint4 *>(p.vc + (size_t)i * 8);
     }
-}
-
-// scale_a v_t, rank i: the K groups' sums in order.
-__device__ __forceinline__ float low_rank(const AdapterParams &p, int id, int t, int i)
-{
-    float v = 0.f;
-    for (int g = 0; g < p.vgroups; ++g) v += p.v[((size_t)g * p.T + t) * p.r + i];
-    return v * scale_of(p, id);
-}
-// (B_a)_i v over the r ranks.
-__device__ __forceinline__ float expand(const AdapterParams &p, int id, int i, const float *v)
-{
-    const uint4 *b = reinterpret_cast<const uint4 *>(p.b + ((size_t)id * p.o + i) * p.r * 2);
-    float s = 0.f;
-#pragma unroll 4
-    for (int c = 0; c < p.r / 8; ++c) {
-        const uint4 q = b[c];
-        const float *u = v + c * 8;
-        s = fmaf(__uint_as_float(q.x << 16), u[0], s);
-        s = fmaf(__uint_as_float(q.x & 0xffff0000u), u[1], s);
-        s = fmaf(__uint_as_float(q.y << 16), u[2], s);
-        s = fmaf(__uint_as_float(q.y & 0xffff0000u), u[3], s);
-        s = fmaf(__uint_as_float(q.z << 16), u[4], s);
-        s = fmaf(__uint_as_float(q.z & 0xffff0000u), u[5], s);
-        s = fmaf(__uint_as_float(q.w << 16), u[6], s);
-        s = fmaf(__uint_as_float(q.w & 0xffff0000u), u[7], s);
-    }
-    return s;
-}
-
-struct RowsSrc {
-    const uint8_t *base0, *base1;
-    size_t half;
-    int c0, cnt;
-    const AdapterParams &p;
-    int it, end, rbs, group, wv;
-    int s;   // chunks of a unit
-    template <class R>
-    __device__ __forceinline__ bool next(R &)
-    {
-        const int C = (p.d + kChunk - 1) / kChunk, units = (C + s - 1) / s;
-        for (;;) {
-            if (it >= end) return false;
-            const int g = it / rbs;
-            if (g != group) {
-                group = g;
-                const int u = g * kWaves + wv;
-                c0 = cnt = 0;
-                if (u < units) part_chunks(C, u, units, c0, cnt);
-            }
-            if (cnt) break;
-            it = (g + 1) * rbs;   // nothing for this wave in the group
-        }
-        const int rb = it - group * rbs;
-        const size_t K2 = (size_t)p.d * 2;
-        base0 = p.w + (size_t)rb * kRows * K2;
-        half = rb * kRows + 8 < p.o ? 8 * K2 : 0;
-        ++it;
-        return true;
-    }
-};
-
-// W x for up to 16 tokens. A work group takes an equal, contiguous share of the (group, 16 rows)
-// items. kOne: there is one group, and the adapters' part, y_in and the rounding follow here.
-template <int S, int NB, bool kOne>
-__global__ __launch_bounds__(kThreads) void k_adapter_rows(AdapterParams p)
-{
-    constexpr int RS = NB <= 2 ? 8 : 6;
-    constexpr int kRing = kWaves * RS * kStageBytes;
-    __shared__ __align__(1024) uint8_t lds[kRing + kWaves * NB * 1024];
-    __shared__ float v[kOne ? kStreamTokens * MOE_ADAPTER_MAX_RANK : 1];
-    const int tid = threadIdx.x, wv = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int rbs = (p.o + kRows - 1) / kRows;
+    const int units = p.w ? (chunks_of(p.d) + S - 1) / S : 0;
     const int64_t total = (int64_t)p.groups * rbs;
     const int it0 = (int)(total * blockIdx.x / gridDim.x), it1 = (int)(total * (blockIdx.x + 1) / gridDim.x);
-    RowsSrc src{nullptr, nullptr, 0, 0, 0, p, it0, it1, rbs, -1, wv, S};
-    Stream<S, 1, NB, RS, RowsSrc> st;
-    st.ring.row_bytes((int64_t)p.d * 2);
-    st.start(src, lds + wv * RS * kStageBytes);
-    if (kOne) {
-        for (int i = tid; i < p.T * p.r; i += kThreads) {
-            const int t = i / p.r, id = p.ids[t];
-            v[i] = has_adapter(p, id) ? low_rank(p, id, t, i - t * p.r) : 0.f;
-        }
-        __syncthreads();
-    }
-    float *red = reinterpret_cast<float *>(lds + kRing);
-    const int parts = p.bf16 ? 1 : 3;
-    const int row = tid & 15, t = tid >> 4;
-    const int id = kOne && t < p.T ? p.ids[t] : -1;
+    const int parts = x_parts(p.bf16), cols = p.T * parts;
+    int group = it0 / rbs, c0, cnt;
+    unit_chunks(chunks_of(p.d), group * kWaves + wv, units, c0, cnt);
     bf16x8_t bx[S][2][NB];
-    int group = -1, c0 = 0, cnt = 0;
-    for (int it = it0; it < it1; ++it) {
-        const int g = it / rbs, rb = it - g * rbs;
+    load_columns<S, NB, STK>(p.xc + (size_t)c0 * (kChunk / 8) * cols * 16, cols, p.T, cnt, bx);
+    settle(bx);
+    __syncthreads();
+    const int adapters = __builtin_amdgcn_readfirstlane(nlist);
+    const int mine0 = wv < adapters ? list[wv] : -1, mine1 = wv + kWaves < adapters ? list[wv + kWaves] : -1;
+    RowsSrc<S> src{p, list, wv, it0, it1, rbs, units, adapters, {}};
+    src.r.w.bytes = p.d * 2;
+    src.r.w.lane_row = lane_row_of(p.d * 2);
+    src.r.bbytes = p.r * 2;
+    src.r.blane = lane_row_of(p.r * 2);
+    src.r.rc = rc;
+    Stream_t st;
+    st.start(src, lds + wv * Stream_t::kBytes, p.xc);
+    auto output = [&](int t, int row, float s) {
+        if (p.y_in) s += load_act(p.y_in, p.bf16, (size_t)t * p.ldyin + row);
+        store_act(p.y, p.bf16, (size_t)t * p.ldy + row, s);
+    };
+    const uint32_t v_at = lds_address(v) + ((lane & 15) * kRankPitch + (lane >> 4) * 8) * 2;
+    const Partials partials{p.partial, p.counts, kept, kKeptSums, p.groups, rbs, p.o, p.T, it0, it1};
+    for (int it = it0, n = 0; it < it1; ++it, ++n) {
+        const int g = it / rbs;
         if (g != group) {
             group = g;
-            group_chunks<S>(p.d, g, wv, c0, cnt);
-            load_tokens<S, NB>(p, 0, p.T, c0, cnt, bx);
+            unit_chunks(chunks_of(p.d), g * kWaves + wv, units, c0, cnt);
+            load_columns<S, NB, STK>(p.xc + (size_t)c0 * (kChunk / 8) * cols * 16, cols, p.T, cnt, bx);
+            settle(bx);
         }
-        floatx4_t acc[1][NB];
-        st.item(src, bx, cnt, acc);
-        lds_barrier();
-        put_sums(red, wv, acc);
-        lds_barrier();
-        const int i = rb * kRows + row;
-        if (t < p.T && i < p.o) {
-            float s = 0.f;
-            for (int q = 0; q < parts; ++q) s += get_sum<1, NB>(red, 0, row, q * p.T + t);
-            if (kOne) {
-                if (p.y_in) s += load_act(p.y_in, p.bf16, (size_t)t * p.ldyin + i);
-                if (has_adapter(p, id)) s += expand(p, id, i, v + t * p.r);
-                store_act(p.y, p.bf16, (size_t)t * p.ldy + i, s);
-            } else {
-                p.partial[((size_t)g * p.T + t) * p.o + i] = s;
+        floatx4_t acc[AB];
+        clear(acc);
+        multiply<S, NB, STK>(st, bx, cnt, acc);
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            bf16x8_t b[2];
+            st.take(S + e, b);
+            const int second = e >= rc ? 1 : 0, a = g > 0 || e >= 2 * rc ? -1 : second ? mine1 : mine0;
+            if (a < 0) continue;
+            // all the v against this adapter's rows; the others' tokens drop the products, which
+            // their own v would only make wrong numbers of, but another's weights could make NaN
+            const uint32_t at = v_at + (e - second * rc) * (kChunk * 2);
+            floatx4_t d = floatx4_t{0.f, 0.f, 0.f, 0.f};
+            for (int q = 0; q < vp; ++q) {
+                bf16x8_t f[2];
+                asm volatile("ds_read_b128 %0, %2\n\tds_read_b128 %1, %2 offset:64\n\ts_waitcnt lgkmcnt(0)"
+                             : "=&v"(f[0]), "=&v"(f[1])
+                             : "v"(at + q * (kStreamTokens * kRankPitch * 2))
+                             : "memory");
+                d = __builtin_amdgcn_mfma_f32_16x16x32_bf16(b[0], f[0], d, 0, 0, 0);
+                d = __builtin_amdgcn_mfma_f32_16x16x32_bf16(b[1], f[1], d, 0, 0, 0);
             }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) acc[0][i] += own == a ? d[i] : 0.f;
         }
+        st.advance(src);
+        const int out = sums.exchange(n, p.T * kRows, acc);
+        if (out < 0) continue;
+        const int row = out & 15, t = out >> 4;
+        if (t < p.T) partials.put(it, t, row, sums.template token<STK>(n, row, t, p.T, parts), output);
     }
-}
-
-// y of token blockIdx.y, 256 outputs: the groups' sums in order, y_in, the adapter's part.
-__global__ __launch_bounds__(256) void k_adapter_finish(AdapterParams p)
-{
-    __shared__ float v[MOE_ADAPTER_MAX_RANK];
-    const int t = blockIdx.y, i = blockIdx.x * 256 + threadIdx.x, id = p.ids[t];
-    const bool has = has_adapter(p, id);
-    if (has && (int)threadIdx.x < p.r) v[threadIdx.x] = low_rank(p, id, t, threadIdx.x);
-    __syncthreads();
-    if (i >= p.o) return;
-    float s = 0.f;
-#pragma unroll 4
-    for (int g = 0; g < p.groups; ++g) s += p.partial[((size_t)g * p.T + t) * p.o + i];
-    if (p.y_in) s += load_act(p.y_in, p.bf16, (size_t)t * p.ldyin + i);
-    if (has) s += expand(p, id, i, v);
-    store_act(p.y, p.bf16, (size_t)t * p.ldy + i, s);
+    st.end();
+    partials.combine(todo, output);
 }
 
 // ------------------------------------------------------------------ longer batches
@@ -313,77 +320,168 @@ constexpr int kMaxParts = 64;        // part buffers per XCD
 constexpr size_t kPartBytes = (size_t)64 << 20;     // all of them, at most
 constexpr int kStagger = 2;          // K steps between the starts of neighbouring N tiles
 
+// The activations' bf16 parts, K step by K step with zeros to the last one's end: [T][parts][nk * kBK].
+__global__ __launch_bounds__(256) void k_adapter_cast(AdapterParams p, uint16_t *xk)
+{
+    const int per = (int)(p.kpart / 8), parts = x_parts(p.bf16), t = blockIdx.y;
+    const int i = blockIdx.x * 256 + threadIdx.x;
+    if (i >= parts * per) return;
+    const int q = i / per, k = (i - q * per) * 8;
+    const uint4 v = k < p.d ? act_part(p, (size_t)t * p.ldx + k, q) : make_uint4(0, 0, 0, 0);
+    *reinterpret_cast<uint4 *>(xk + (size_t)t * p.ldk + (size_t)q * p.kpart + k) = v;
+}
+
+// The distinct adapters among `n` tokens (up to 64 K), in order of first appearance, by one wave.
+template <int K>
+__device__ __forceinline__ int distinct(const AdapterParams &p, int t0, int n, int32_t *list)
+{
+    const int lane = threadIdx.x & 63;
+    int id[K], count = 0;
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+        const int i = k * kWave + lane;
+        id[k] = i < n ? p.ids[t0 + i] : -1;
+        if (!has_adapter(p, id[k])) id[k] = -1;
+    }
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+        uint64_t m = __ballot(id[k] >= 0);
+        while (m) {
+            const int a = __builtin_amdgcn_readlane(id[k], __builtin_ctzll(m));
+            if (lane == 0) list[count] = a;
+            ++count;
+#pragma unroll
+            for (int j = k; j < K; ++j) id[j] = id[j] == a ? -1 : id[j];
+            m = __ballot(id[k] >= 0);
+        }
+    }
+    return count;
+}
+
+// The B operand's fragments of chunks [c0, c0 + cnt) of tokens t0 .. t0 + tn, from xk.
+template <int S, int NB, bool STK>
+__device__ __forceinline__ void load_tokens(const AdapterParams &p, int t0, int tn, int c0, int cnt, bf16x8_t (&bx)[S][2][NB])
+{
+    const int lane = threadIdx.x & 63, parts = x_parts(p.bf16);
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb) {
+        const int c = nb * 16 + (lane & 15), q = STK ? nb : c / tn, t = STK ? lane & 15 : c - q * tn;
+        const uint16_t *src = p.xk + (size_t)(t0 + t) * p.ldk + (size_t)q * p.kpart + c0 * kChunk + (lane >> 4) * 8;
+#pragma unroll
+        for (int s = 0; s < S; ++s) bx[s][0][nb] = bx[s][1][nb] = no_tokens();
+        if (q < parts && t < tn) {
+#pragma unroll
+            for (int s = 0; s < S; ++s) {
+                if (s < cnt) {
+                    bx[s][0][nb] = *reinterpret_cast<const bf16x8_t *>(src + s * kChunk);
+                    bx[s][1][nb] = *reinterpret_cast<const bf16x8_t *>(src + s * kChunk + 32);
+                }
+            }
+        }
+    }
+}
+
+struct ShrinkSrc {
+    const AdapterParams &p;
+    const int *list;
+    int it, step, total, rbs, cnt;
+    Rows r;
+    __device__ __forceinline__ Rows next()
+    {
+        r.cnt = it < total ? cnt : 0;
+        if (it < total) {
+            const int j = it / rbs, rb = it - j * rbs;
+            r.base = p.a + ((size_t)list[j] * p.r + (size_t)rb * kRows) * r.bytes;
+            r.half = rb * kRows + 8 < p.r ? (size_t)8 * r.bytes : 0;   // the last block may have 8 rows
+            it += step;
+        }
+        return r;
+    }
+};
+
+// v of the tokens of block x, K group y; of the block's (adapter, 16 rows) items every gridDim.z-th.
+template <int S, int NB>
+__global__ __launch_bounds__(kThreads) void k_adapter_shrink(AdapterParams p)
+{
+    constexpr bool STK = NB == 3;
+    constexpr int AB = STK ? 1 : NB;
+    using Stream_t = Stream<S, ShrinkSrc>;
+    __shared__ __align__(1024) uint8_t lds[kWaves * Stream_t::kBytes];
+    __shared__ __align__(16) Sums<AB> sums;
+    __shared__ int32_t list[kBlockTokens];
+    __shared__ int mine[kBlockTokens], njobs;
+    const int tid = threadIdx.x, wv = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int t0 = blockIdx.x * p.tb, tn = min(p.tb, p.T - t0), g = blockIdx.y;
+    if (tid < kWave) {
+        mine[tid] = tid < tn ? p.ids[t0 + tid] : -1;
+        const int n = distinct<1>(p, t0, tn, list);
+        if (tid == 0) njobs = n;
+    }
+    __syncthreads();
+    const int rbs = (p.r + kRows - 1) / kRows, total = __builtin_amdgcn_readfirstlane(njobs) * rbs;
+    if ((int)blockIdx.z >= total) return;
+    const int units = (chunks_of(p.d) + S - 1) / S;
+    ShrinkSrc src{p, list, (int)blockIdx.z, (int)gridDim.z, total, rbs, 0, {}};
+    unit_chunks(chunks_of(p.d), g * kWaves + wv, units, src.r.c0, src.cnt);
+    src.r.bytes = p.d * 2;
+    src.r.lane_row = lane_row_of(p.d * 2);
+    const int cnt = src.cnt, parts = x_parts(p.bf16);
+    bf16x8_t bx[S][2][NB];
+    load_tokens<S, NB, STK>(p, t0, tn, src.r.c0, cnt, bx);
+    settle(bx);
+    Stream_t st;
+    st.start(src, lds + wv * Stream_t::kBytes, reinterpret_cast<const uint8_t *>(p.xk));
+    for (int it = blockIdx.z, n = 0; it < total; it += gridDim.z, ++n) {
+        floatx4_t acc[AB];
+        clear(acc);
+        multiply<S, NB, STK>(st, bx, cnt, acc);
+        st.advance(src);
+        // (all waves make results: up to 64 tokens of 16 rows)
+        (void)sums.exchange(n, kThreads, acc);
+        const int j = it / rbs, row = tid & 15, i = (it - j * rbs) * kRows + row;
+        for (int t = tid >> 4; t < tn; t += kThreads / kRows)
+            if (i < p.r && mine[t] == list[j])
+                p.v[((size_t)g * p.T + t0 + t) * p.r + i] = sums.template token<STK>(n, row, t, tn, parts);
+    }
+    st.end();
+}
+
 struct GemmParams {
     AdapterParams p;
-    const uint16_t *xk;       // activations in bf16, K steps side by side: [T][ldk]
-    int64_t ldk;
     int nk, steps;            // K steps of W; of a tile (times the activations' parts)
-    const uint16_t *vk;       // v in bf16, [T][vparts][rq * 64]
+    uint16_t *vk;             // v in bf16, [T][vparts][rq * kBK]
     int vparts, rq;           // parts of v, K steps of its ranks
-    const uint16_t *zeros;    // kBK zeros
-    const int32_t *list;      // [mtiles][1 + kTileM] adapters of a tile: count, ids
+    int32_t *list;            // [mtiles][1 + kTileM] adapters of a tile: count, ids
     int mtiles, ntiles, slots;
     TilePlan plan[kXcds];
     int maxparts, prows;      // part buffers per XCD and their rows
     float *part;              // [8][maxparts][prows][kTileN]
 };
 
-// vk, xk (unless the activations are taken as they are), zeros, and the tiles' lists.
-struct PartsParams {
-    AdapterParams p;
-    uint16_t *vk, *xk, *zeros;
-    int vparts, rq, nk;
-    bool copy;
-    int32_t *list;
-    int mtiles;
-};
-__global__ __launch_bounds__(256) void k_adapter_parts(PartsParams g)
+// The tiles' lists, a wave each; then vk, 256 values of v per work group.
+__global__ __launch_bounds__(256) void k_adapter_parts(GemmParams g)
 {
     const AdapterParams &p = g.p;
-    const int tid = threadIdx.x;
-    int b = blockIdx.x;
-    if (b < g.mtiles) {   // the distinct adapters of tile b: a thread keeps one token's
-        __shared__ int ids[kTileM], n;
-        const int r0 = tile_row(p.T, b), r1 = tile_row(p.T, b + 1);
-        int id = tid < r1 - r0 ? p.ids[r0 + tid] : -1;
-        if (!has_adapter(p, id)) id = -1;
-        ids[tid] = id;
-        if (tid == 0) n = 0;
-        __syncthreads();
-        bool first = id >= 0;   // the first token with its adapter
-        int rank = 0;           // different adapters before its own
-        for (int j = 0; j < tid; ++j) first = first && ids[j] != id;
-        __syncthreads();
-        ids[tid] = first ? id : -1;
-        __syncthreads();
-        for (int j = 0; j < kTileM; ++j) rank += ids[j] >= 0 && ids[j] < id;
+    const int lists = (g.mtiles + 3) / 4, wv = threadIdx.x >> 6;
+    if ((int)blockIdx.x < lists) {
+        const int b = blockIdx.x * 4 + wv;
+        if (b >= g.mtiles) return;
+        const int r0 = tile_row(p.T, b);
         int32_t *list = g.list + (size_t)b * (kTileM + 1);
-        if (first) {
-            list[1 + rank] = id;
-            atomicAdd(&n, 1);
-        }
-        __syncthreads();
-        if (tid == 0) list[0] = n;
-        if (b == 0 && tid < kBK) g.zeros[tid] = 0;
+        const int n = distinct<kTileM / kWave>(p, r0, tile_row(p.T, b + 1) - r0, list + 1);
+        if ((threadIdx.x & 63) == 0) list[0] = n;
         return;
     }
-    // token by token: v's parts, then the activations' 8 at a time
-    b -= g.mtiles;
-    const int t = b;
-    const int id = p.ids[t];
-    const bool has = has_adapter(p, id);
-    for (int i = tid; i < g.rq * kBK; i += 256) {
-        const float v = has && i < p.r ? low_rank(p, id, t, i) : 0.f;
-        for (int q = 0; q < g.vparts; ++q)
-            g.vk[((size_t)t * g.vparts + q) * g.rq * kBK + i] = g.vparts == 3 ? part_of<3>(v, q) : part_of<2>(v, q);
+    const int rp = g.rq * kBK;
+    const int64_t i = (int64_t)(blockIdx.x - lists) * 256 + threadIdx.x;
+    if (i >= (int64_t)p.T * rp) return;
+    const int t = (int)(i / rp), j = (int)(i - (int64_t)t * rp), id = p.ids[t];
+    float v = 0.f;
+    if (has_adapter(p, id) && j < p.r) {
+        for (int k = 0; k < p.vgroups; ++k) v += p.v[((size_t)k * p.T + t) * p.r + j];
+        v *= scale_of(p, id);
     }
-    if (!g.copy) return;
-    const int parts = p.bf16 ? 1 : 3, per = g.nk * kBK / 8;
-    for (int i = tid; i < parts * per; i += 256) {
-        const int q = i / per, k = (i - q * per) * 8;
-        const bf16x8_t v = k < p.d ? load_part(p.x, p.bf16, (size_t)t * p.ldx + k, q) : no_tokens();
-        *reinterpret_cast<bf16x8_t *>(g.xk + ((size_t)t * parts + q) * g.nk * kBK + k) = v;
-    }
+    for (int q = 0; q < g.vparts; ++q) g.vk[((size_t)t * g.vparts + q) * rp + j] = v_part(p.bf16, v, q);
 }
 
 // Rings of a tile of HB * 32 tokens: as many stages as LDS holds.
@@ -443,7 +541,7 @@ __device__ __forceinline__ void project_tile(const GemmParams &g, uint8_t *lds, 
     };
     const uint8_t *asrc[C::kALoads];
 #pragma unroll
-    for (int j = 0; j < C::kALoads; ++j) asrc[j] = reinterpret_cast<const uint8_t *>(g.xk + token_row(j) * g.ldk) + lc;
+    for (int j = 0; j < C::kALoads; ++j) asrc[j] = reinterpret_cast<const uint8_t *>(p.xk + token_row(j) * p.ldk) + lc;
     const uint32_t wlane = (uint32_t)lr * K2;
     auto step_of = [&](int stage) {   // steps go round from `start`
         const int ks = stage + start;
@@ -536,13 +634,15 @@ __device__ __forceinline__ void project_tile(const GemmParams &g, uint8_t *lds, 
     }
 
     if (ext) {
-        // The adapters' steps, two at a time: rows of another adapter (or none) read zeros.
+        // The adapters' steps, two at a time. Every token's v meets every adapter of the tile; a
+        // step's products are added to the tokens of its adapter only (not by zeros in v: one
+        // request's infinite or NaN weights must not reach another's tokens).
         const int32_t *list = g.list + (size_t)mt * (kTileM + 1);
         const int per = g.vparts * g.rq, r2 = p.r * 2;
         const int total = __builtin_amdgcn_readfirstlane(list[0]) * per;
-        int own[C::kALoads];
+        int own[HB];
 #pragma unroll
-        for (int j = 0; j < C::kALoads; ++j) own[j] = p.ids[token_row(j)];
+        for (int m = 0; m < HB; ++m) own[m] = p.ids[row0 + min((wm * HB + m) * 16 + (lane & 15), rows - 1)];
         for (int e = 0; e < total; e += 2) {
             wait_and_barrier<0>();   // what LDS holds is read
 #pragma unroll
@@ -550,10 +650,8 @@ __device__ __forceinline__ void project_tile(const GemmParams &g, uint8_t *lds, 
                 if (e + u >= total) break;
                 const int a = __builtin_amdgcn_readfirstlane(list[1 + (e + u) / per]), q = (e + u) % per, rc = q % g.rq;
 #pragma unroll
-                for (int i = 0; i < C::kALoads; ++i) {
-                    const uint16_t *v = g.vk + ((size_t)token_row(i) * per + q) * kBK;
-                    put_a(i, reinterpret_cast<const uint8_t *>(own[i] == a ? v : g.zeros) + lc, u);
-                }
+                for (int i = 0; i < C::kALoads; ++i)
+                    put_a(i, reinterpret_cast<const uint8_t *>(g.vk + ((size_t)token_row(i) * per + q) * kBK) + lc, u);
 #pragma unroll
                 for (int i = 0; i < kBLoads; ++i)
                     put_b(i, p.b + ((size_t)a * p.o + w_block(i)) * r2 + (uint32_t)(lr * r2 + min(rc * kRowBytes + lc, r2 - 16)), u);
@@ -562,10 +660,27 @@ __device__ __forceinline__ void project_tile(const GemmParams &g, uint8_t *lds, 
 #pragma unroll
             for (int u = 0; u < 2; ++u) {
                 if (e + u >= total) break;
+                const int a = __builtin_amdgcn_readfirstlane(list[1 + (e + u) / per]);
+                bf16x8_t w[2][4];
 #pragma unroll
-                for (int j = 0; j < kItems; ++j) {
-                    read_item(j, u, u);
-                    mma(j, tf[j % R]);
+                for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+                    for (int nb = 0; nb < 4; ++nb)
+                        w[kb][nb] = *reinterpret_cast<const bf16x8_t *>(rb + u * kBBytes + nb * 16 * kRowBytes + (rd ^ (kb * 64)));
+#pragma unroll
+                for (int m = 0; m < HB; ++m) {
+                    bf16x8_t v[2];
+#pragma unroll
+                    for (int kb = 0; kb < 2; ++kb)
+                        v[kb] = *reinterpret_cast<const bf16x8_t *>(ra + u * C::kABytes + m * 16 * kRowBytes + (rd ^ (kb * 64)));
+#pragma unroll
+                    for (int nb = 0; nb < 4; ++nb) {
+                        floatx4_t d = floatx4_t{0.f, 0.f, 0.f, 0.f};
+                        d = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w[0][nb], v[0], d, 0, 0, 0);
+                        d = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w[1][nb], v[1], d, 0, 0, 0);
+#pragma unroll
+                        for (int c = 0; c < 4; ++c) acc[m][nb][c] += own[m] == a ? d[c] : 0.f;
+                    }
                 }
             }
         }
@@ -642,7 +757,7 @@ __global__ __launch_bounds__(kThreads) void k_adapter_gemm(GemmParams g)
 
 // y of the tiles split over K: the parts in order, and y_in. Work group b: XCD b mod 8, split tile
 // i of that XCD, a block of 16 of its rows.
-constexpr int kTailRows = 16;
+constexpr int kTailRows = 4;
 __global__ __launch_bounds__(256) void k_adapter_tail(GemmParams g)
 {
     const AdapterParams &p = g.p;
@@ -652,14 +767,20 @@ __global__ __launch_bounds__(256) void k_adapter_tail(GemmParams g)
     const int t = pl.u0 + pl.full + i, mt = t % g.mtiles, nt = t / g.mtiles;
     const int row0 = tile_row(p.T, mt), rows = tile_row(p.T, mt + 1) - row0;
     const float *part = g.part + ((size_t)xcd * g.maxparts + (size_t)i * pl.s) * g.prows * kTileN;
-    for (int c = threadIdx.x; c < kTailRows * kTileN; c += 256) {
-        const int tr = rb * kTailRows + c / kTileN, col = c % kTileN, o = nt * kTileN + col;
+    constexpr int kQuads = kTileN / 4;
+    for (int c = threadIdx.x; c < kTailRows * kQuads; c += 256) {
+        const int tr = rb * kTailRows + c / kQuads, col = c % kQuads * 4, o = nt * kTileN + col;
         if (tr >= rows || o >= p.o) continue;
-        float s = 0.f;
-        for (int j = 0; j < pl.s; ++j) s += part[((size_t)j * g.prows + tr) * kTileN + col];
+        floatx4_t s = floatx4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+        for (int j = 0; j < pl.s; ++j) s += *reinterpret_cast<const floatx4_t *>(part + ((size_t)j * g.prows + tr) * kTileN + col);
         const size_t tok = row0 + tr;
-        if (p.y_in) s += load_act(p.y_in, p.bf16, tok * p.ldyin + o);
-        store_act(p.y, p.bf16, tok * p.ldy + o, s);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            float v = s[k];
+            if (p.y_in) v += load_act(p.y_in, p.bf16, tok * p.ldyin + o + k);
+            store_act(p.y, p.bf16, tok * p.ldy + o + k, v);
+        }
     }
 }
 
@@ -667,59 +788,62 @@ __global__ __launch_bounds__(256) void k_adapter_tail(GemmParams g)
 size_t a256(size_t v) { return (v + 255) & ~(size_t)255; }
 int ceil_div(int64_t a, int64_t b) { return (int)((a + b - 1) / b); }
 
-// A token-block product's shape: column blocks and chunks of a unit (row_stream.h), groups of the
-// d columns. The fragments take 8 NB S registers.
+// A token-block product's shape: column blocks, chunks of a unit (row_stream.h), groups of the
+// K columns. Units of up to 8 chunks (4 with three column blocks or more, whose fragments fill the
+// registers), as few groups as those make, all units alike.
 struct StreamPlan {
     int nb, s, groups;
 };
-StreamPlan stream_plan(int d, int cols)
+StreamPlan stream_plan(int d, int parts, int tokens)
 {
     StreamPlan q{};
-    q.nb = ceil_div(cols, 16);
-    q.s = q.nb <= 2 ? 8 : 4;
-    const int chunks = ceil_div(d, kChunk);
-    while (q.s > 1 && chunks <= q.s / 2 * kWaves) q.s /= 2;
-    q.groups = ceil_div(ceil_div(chunks, q.s), kWaves);
+    q.nb = column_blocks(parts, tokens);
+    if (parts == 1 && q.nb == 3) q.nb = 4;   // (three blocks are stacked parts)
+    const int chunks = chunks_of(d);
+    q.groups = ceil_div(ceil_div(chunks, q.nb <= 2 ? 8 : 4), kWaves);
+    q.s = ceil_div(chunks, q.groups * kWaves);
     return q;
 }
 
 struct AdapterPlan {
-    int tb;                    // tokens of a shrink block
-    StreamPlan shrink, rows;
-    bool gemm;
-    int vparts, rq, nk, mtiles, prows, maxparts;
-    size_t v, partial, vk, xk, zeros, list, part, bytes;
+    StreamPlan stream;         // of the rows (up to 16 tokens) or of shrink
+    bool gemm, copy;
+    int tb, nk, vparts, rq, mtiles, prows, maxparts;
+    size_t xc, vc, partial, counts;            // up to 16 tokens
+    size_t xk, v, vk, list, part, bytes;       // longer
 };
 
 AdapterPlan plan_adapter(int T, int d, int o, int r, bool bf16)
 {
     AdapterPlan L{};
-    const int parts = bf16 ? 1 : 3;
-    L.gemm = T > kStreamTokens;
-    // 64 columns of bf16 tokens, 48 of fp32 ones: an adapter's rows are read once per block
-    L.tb = std::min(T, bf16 ? kBlockTokens : kStreamTokens);
-    L.shrink = stream_plan(d, L.tb * parts);
-    L.rows = stream_plan(d, std::min(T, kStreamTokens) * parts);
-    // v meets B in three exact parts; beside bf16 activations in two (2^-17 relative)
-    L.vparts = bf16 ? 2 : 3;
-    L.rq = ceil_div(r, kBK);
-    L.nk = ceil_div(d, kBK);
-    L.mtiles = tiles_of(T);
-    L.prows = std::min(T, kTileM);
-    L.maxparts = (int)std::min<size_t>(kMaxParts, kPartBytes / ((size_t)kXcds * L.prows * kTileN * 4));
+    const int parts = x_parts(bf16);
     size_t at = 0;
     auto take = [&](size_t b) {
         const size_t was = at;
         at += a256(b);
         return was;
     };
-    L.v = take((size_t)L.shrink.groups * T * r * 4);
+    L.vparts = v_parts(bf16);
+    L.gemm = T > kStreamTokens;
     if (!L.gemm) {
-        L.partial = take(L.rows.groups > 1 ? (size_t)L.rows.groups * T * o * 4 : 0);
+        L.stream = stream_plan(d, parts, T);
+        L.xc = take((size_t)chunks_of(d) * kChunk * T * parts * 2);
+        L.vc = take((size_t)L.vparts * T * chunks_of(r) * kChunk * 2);
+        L.partial = take(L.stream.groups > 1 ? (size_t)L.stream.groups * T * o * 4 : 0);
+        L.counts = take((size_t)ceil_div(o, kRows) * 4);
     } else {
+        // 64 bf16 tokens or 16 fp32 ones to a shrink block: an adapter's rows are read once per block
+        L.tb = std::min(T, bf16 ? kBlockTokens : kStreamTokens);
+        L.stream = stream_plan(d, parts, L.tb);
+        L.nk = ceil_div(d, kBK);
+        L.copy = !bf16 || d % kBK != 0;   // bf16 rows that end with a K step are read where they are
+        L.rq = ceil_div(r, kBK);
+        L.mtiles = tiles_of(T);
+        L.prows = std::min(T, kTileM);
+        L.maxparts = (int)std::min<size_t>(kMaxParts, kPartBytes / ((size_t)kXcds * L.prows * kTileN * 4));
+        L.xk = take(L.copy ? (size_t)T * parts * L.nk * kBK * 2 : 0);
+        L.v = take((size_t)L.stream.groups * T * r * 4);
         L.vk = take((size_t)T * L.vparts * L.rq * kBK * 2);
-        L.xk = take((size_t)T * parts * L.nk * kBK * 2);
-        L.zeros = take(kRowBytes);
         L.list = take((size_t)L.mtiles * (kTileM + 1) * 4);
         L.part = take((size_t)kXcds * L.maxparts * L.prows * kTileN * 4);
     }
@@ -728,99 +852,113 @@ AdapterPlan plan_adapter(int T, int d, int o, int r, bool bf16)
 }
 
 template <int S, int NB>
-hipError_t launch_shrink(const AdapterParams &p, hipStream_t s, dim3 grid)
-{
-    hipLaunchKernelGGL((k_adapter_shrink<S, NB>), grid, dim3(kThreads), 0, s, p);
-    return hipGetLastError();
-}
-template <int S, int NB>
 hipError_t launch_rows(const AdapterParams &p, hipStream_t s)
 {
     const dim3 grid((unsigned)std::min<int64_t>(device_cu_count(), (int64_t)p.groups * ceil_div(p.o, kRows)));
-    if (p.groups == 1) hipLaunchKernelGGL((k_adapter_rows<S, NB, true>), grid, dim3(kThreads), 0, s, p);
-    else hipLaunchKernelGGL((k_adapter_rows<S, NB, false>), grid, dim3(kThreads), 0, s, p);
+    // stages of B: a wave has one adapter per 8 tokens, and a stage per 64 ranks
+    if (ceil_div(p.T, kWaves) * ceil_div(p.r, kChunk) <= 2) hipLaunchKernelGGL((k_adapter_rows<S, 2, NB>), grid, dim3(kThreads), 0, s, p);
+    else hipLaunchKernelGGL((k_adapter_rows<S, 4, NB>), grid, dim3(kThreads), 0, s, p);
     return hipGetLastError();
 }
 
-#define MOE_STREAM_CASES(F)                                                                                   \
-    F(1, 1) F(1, 2) F(1, 4) F(1, 8) F(2, 1) F(2, 2) F(2, 4) F(2, 8) F(3, 1) F(3, 2) F(3, 4)
-
-hipError_t launch_adapter(AdapterParams p, const AdapterPlan &L, uint8_t *ws, hipStream_t s)
+hipError_t launch_decode(AdapterParams p, const AdapterPlan &L, uint8_t *ws, hipStream_t s)
 {
-    (void)hipGetLastError();
-    hipError_t e = hipSuccess;
+    p.xc = ws + L.xc;
+    p.vc = reinterpret_cast<uint16_t *>(ws + L.vc);
+    p.partial = reinterpret_cast<float *>(ws + L.partial);
+    p.counts = reinterpret_cast<uint32_t *>(ws + L.counts);
+    p.groups = p.w ? L.stream.groups : 1;
+    const int rows = p.T * ceil_div(p.r, kChunk) * kChunk;
+    const int split = rows <= 4 * device_cu_count() ? 4 : 1;
+    const int v_blocks = ceil_div(rows, 4 / split), c_blocks = ceil_div((int64_t)chunks_of(p.d) * (kChunk / 8) * p.T * x_parts(p.bf16), 256);
+    hipLaunchKernelGGL(k_adapter_prepare, dim3((unsigned)(v_blocks + c_blocks)), dim3(256), 0, s, p, split, v_blocks);
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    switch (L.stream.nb * 100 + L.stream.s) {
+#define MOE_CASE(NB, S) \
+    case NB * 100 + S: return launch_rows<S, NB>(p, s);
+        MOE_CASE(1, 1) MOE_CASE(1, 2) MOE_CASE(1, 3) MOE_CASE(1, 4) MOE_CASE(1, 5) MOE_CASE(1, 6) MOE_CASE(1, 7) MOE_CASE(1, 8)
+        MOE_CASE(2, 1) MOE_CASE(2, 2) MOE_CASE(2, 3) MOE_CASE(2, 4) MOE_CASE(2, 5) MOE_CASE(2, 6) MOE_CASE(2, 7) MOE_CASE(2, 8)
+        MOE_CASE(3, 1) MOE_CASE(3, 2) MOE_CASE(3, 3) MOE_CASE(3, 4)
+#undef MOE_CASE
+    default: return hipErrorInvalidValue;
+    }
+}
+
+hipError_t launch_shrink(const AdapterParams &p, const AdapterPlan &L, hipStream_t s)
+{
+    const int blocks = ceil_div(p.T, L.tb), items = std::min(L.tb, p.n) * ceil_div(p.r, kRows);
+    // enough work groups for the chip; a block's items are shared out among them
+    const int split = std::max(1, std::min(items, 2 * device_cu_count() / (blocks * L.stream.groups)));
+    const dim3 grid((unsigned)blocks, (unsigned)L.stream.groups, (unsigned)split);
+    switch (L.stream.nb * 100 + L.stream.s) {
+#define MOE_CASE(NB, S) \
+    case NB * 100 + S: hipLaunchKernelGGL((k_adapter_shrink<S, NB>), grid, dim3(kThreads), 0, s, p); break;
+        MOE_CASE(2, 1) MOE_CASE(2, 2) MOE_CASE(2, 3) MOE_CASE(2, 4) MOE_CASE(2, 5) MOE_CASE(2, 6) MOE_CASE(2, 7) MOE_CASE(2, 8)
+        MOE_CASE(3, 1) MOE_CASE(3, 2) MOE_CASE(3, 3) MOE_CASE(3, 4)
+        MOE_CASE(4, 1) MOE_CASE(4, 2) MOE_CASE(4, 3) MOE_CASE(4, 4)
+#undef MOE_CASE
+    default: return hipErrorInvalidValue;
+    }
+    return hipGetLastError();
+}
+
+// K parts of the tiles of an XCD's last round: r tiles of `steps` K steps on `slots` work groups. A
+// part costs a few K steps to start, and its sums are written and read again: 2 KiB a row against
+// the (rows + 256) * 128 bytes of a K step.
+int split_of(int r, int steps, int slots, int maxparts, int rows)
+{
+    if (r == 0) return 1;
+    int best = 1, least = steps;
+    for (int s = 2; s <= kMaxSplit && s * kMinPartSteps <= steps && r * s <= maxparts; ++s) {
+        const int cost = ceil_div(r * s, slots) * (ceil_div(steps, s) + 2 + 16 * rows / (rows + kTileN)) + 8;
+        if (cost < least) {
+            least = cost;
+            best = s;
+        }
+    }
+    return best;
+}
+
+hipError_t launch_gemm(AdapterParams p, const AdapterPlan &L, uint8_t *ws, hipStream_t s)
+{
+    hipError_t e;
+    const int parts = x_parts(p.bf16);
+    const bool copy = L.copy && (p.w || p.n > 0);
+    uint16_t *xk = reinterpret_cast<uint16_t *>(ws + L.xk);
+    p.xk = L.copy ? xk : static_cast<const uint16_t *>(p.x);
+    p.kpart = L.copy ? (int64_t)L.nk * kBK : 0;
+    p.ldk = L.copy ? parts * p.kpart : p.ldx;
     p.tb = L.tb;
     p.v = reinterpret_cast<float *>(ws + L.v);
-    p.vgroups = L.shrink.groups;
-    if (p.n > 0) {
-        const int blocks = ceil_div(p.T, L.tb), items = std::min(L.tb, p.n) * ceil_div(p.r, kRows);
-        // enough work groups for the chip; a block's items are shared out among them
-        const int split = std::max(1, std::min(items, 2 * device_cu_count() / (blocks * L.shrink.groups)));
-        const dim3 grid(blocks, L.shrink.groups, split);
-        switch (L.shrink.nb * 100 + L.shrink.s) {
-#define MOE_CASE(NB, S) \
-    case NB * 100 + S: e = launch_shrink<S, NB>(p, s, grid); break;
-            MOE_STREAM_CASES(MOE_CASE) MOE_CASE(4, 1) MOE_CASE(4, 2) MOE_CASE(4, 4)
-#undef MOE_CASE
-        default: return hipErrorInvalidValue;
-        }
-        if (e != hipSuccess) return e;
+    p.vgroups = L.stream.groups;
+    if (copy) {
+        hipLaunchKernelGGL(k_adapter_cast, dim3((unsigned)ceil_div(parts * p.kpart / 8, 256), (unsigned)p.T), dim3(256), 0, s, p, xk);
+        if ((e = hipGetLastError()) != hipSuccess) return e;
     }
-    if (!L.gemm) {
-        p.groups = p.w ? L.rows.groups : 0;
-        p.partial = reinterpret_cast<float *>(ws + L.partial);
-        if (p.w) {
-            switch (L.rows.nb * 100 + L.rows.s) {
-#define MOE_CASE(NB, S) \
-    case NB * 100 + S: e = launch_rows<S, NB>(p, s); break;
-                MOE_STREAM_CASES(MOE_CASE)
-#undef MOE_CASE
-            default: return hipErrorInvalidValue;
-            }
-            if (e != hipSuccess || p.groups == 1) return e;
-        }
-        hipLaunchKernelGGL(k_adapter_finish, dim3((unsigned)ceil_div(p.o, 256), (unsigned)p.T), dim3(256), 0, s, p);
-        return hipGetLastError();
-    }
-    PartsParams q{};
-    q.p = p;
-    q.vk = reinterpret_cast<uint16_t *>(ws + L.vk);
-    q.xk = reinterpret_cast<uint16_t *>(ws + L.xk);
-    q.zeros = reinterpret_cast<uint16_t *>(ws + L.zeros);
-    q.list = reinterpret_cast<int32_t *>(ws + L.list);
-    q.vparts = L.vparts;
-    q.rq = L.rq;
-    q.nk = L.nk;
-    q.mtiles = L.mtiles;
-    // bf16 rows that end with a K step are read where they are
-    q.copy = p.w && (!p.bf16 || p.d % kBK != 0);
-    hipLaunchKernelGGL(k_adapter_parts, dim3((unsigned)(L.mtiles + p.T)), dim3(256), 0, s, q);
-    if ((e = hipGetLastError()) != hipSuccess) return e;
+    if (p.n > 0 && (e = launch_shrink(p, L, s)) != hipSuccess) return e;
     GemmParams g{};
-    const int parts = p.bf16 ? 1 : 3;
     g.p = p;
-    g.xk = q.copy ? q.xk : static_cast<const uint16_t *>(p.x);
-    g.ldk = q.copy ? (int64_t)parts * L.nk * kBK : p.ldx;
     g.nk = L.nk;
     g.steps = p.w ? parts * L.nk : 0;
-    g.vk = q.vk;
+    g.vk = reinterpret_cast<uint16_t *>(ws + L.vk);
     g.vparts = L.vparts;
     g.rq = L.rq;
-    g.zeros = q.zeros;
-    g.list = q.list;
+    g.list = reinterpret_cast<int32_t *>(ws + L.list);
     g.mtiles = L.mtiles;
     g.ntiles = ceil_div(p.o, kTileN);
     g.slots = std::max(1, device_cu_count() / kXcds);
     g.maxparts = L.maxparts;
     g.prows = L.prows;
     g.part = reinterpret_cast<float *>(ws + L.part);
+    const int v_blocks = ceil_div((int64_t)p.T * L.rq * kBK, 256);
+    hipLaunchKernelGGL(k_adapter_parts, dim3((unsigned)(ceil_div(L.mtiles, 4) + v_blocks)), dim3(256), 0, s, g);
+    if ((e = hipGetLastError()) != hipSuccess) return e;
     const int U = g.mtiles * g.ntiles;
     bool tail = false;
     for (int x = 0; x < kXcds; ++x) {
         const int left = tile_plan(U, g.slots, x, 1).units % g.slots;
-        int best = 0x7fffffff;
-        for (int k = 1; k <= kMaxSplit; ++k) best = std::min(best, split_key(left, g.steps, g.slots, 0, g.maxparts, 0, k));
-        g.plan[x] = tile_plan(U, g.slots, x, best % kMaxSplit + 1);
+        g.plan[x] = tile_plan(U, g.slots, x, split_of(left, g.steps, g.slots, g.maxparts, ceil_div(p.T, g.mtiles)));
         tail = tail || (g.plan[x].s > 1 && g.plan[x].units > g.plan[x].full);
     }
     const dim3 grid(kXcds * g.slots);
@@ -829,6 +967,12 @@ hipError_t launch_adapter(AdapterParams p, const AdapterPlan &L, uint8_t *ws, hi
     if ((e = hipGetLastError()) != hipSuccess || !tail) return e;
     hipLaunchKernelGGL(k_adapter_tail, dim3((unsigned)(kXcds * g.slots * ceil_div(g.prows, kTailRows))), dim3(256), 0, s, g);
     return hipGetLastError();
+}
+
+hipError_t launch_adapter(const AdapterParams &p, const AdapterPlan &L, uint8_t *ws, hipStream_t s)
+{
+    (void)hipGetLastError();
+    return L.gemm ? launch_gemm(p, L, ws, s) : launch_decode(p, L, ws, s);
 }
 
 }  // namespace

@@ -4,17 +4,16 @@
 //   FFN(x) = W2 (SiLU(W1 x) * W3 x)
 //
 // Every selected expert's weights are read once for all the tokens. Kernels, on one stream:
-//   1. logits: fp64 sums, one wave per (token, expert);
-//   2. gate/up: each work group selects the top k from the logits and then takes blocks of 16
-//      rows of W1 and W3 of the selected experts and of the shared one. All the tokens are
-//      multiplied with every expert's rows (the matrix cores have room for 16 columns whether
-//      they are used or not), so the tokens' fragments are loaded once per work group. The
+//   1. prepare: the logits in fp64, and x as operand columns;
+//   2. gate/up: each work group selects the top k from the logits and then takes blocks of 8
+//      rows of W1 and the same 8 of W3, of the shared expert and of the selected ones. All the
+//      tokens are multiplied with every expert's rows (the matrix cores have room for 16 columns
+//      whether they are used or not), so the tokens' fragments are loaded once per work group. The
 //      hidden values of a token that did not select the expert are zero, the others are scaled
 //      by the gate weight, so that
 //   3. down is one sum over all the experts' hidden columns, y_t = W2_all h_t: the columns are
 //      cut into units of up to 512, a work group takes eight units (a group) of 16 rows of W2,
-//      and, where there is more than one group,
-//   4. the groups' sums are added in order.
+//      and the last one to end a block of rows adds its groups in order.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -44,16 +43,17 @@ struct LayerParams {
     double *logits;               // [T][n]
     int32_t *idx;                 // [T][k]
     float *w;                     // [T][k]
-    uint8_t *h;                   // hidden values as operand fragments (h_offset)
-    int cols;                     // columns of h: T times its parts
+    uint8_t *xc, *h;              // x and the hidden values as columns (row_stream.h); h job after job, the shared expert's first
     float *partial;               // [groups][T][d]
+    uint32_t *counts;             // [row blocks of y]
     const void *y_in;             // or null
     void *y;
 };
 
-// Part counts: fp32 activations and hidden values in three parts (exact); for a bf16 layer x is
-// exact in one, and the hidden values are kept in two (2^-17 relative: far below the rounding
-// of y, at the cost of columns that are there anyway).
+// Parts: fp32 activations and hidden values in three (exact); for a bf16 layer x is exact in one, and
+// the hidden values are kept in two (2^-17 relative: far below the rounding of y, at the cost of
+// columns that are there anyway).
+__host__ __device__ inline int x_parts(bool bf16) { return bf16 ? 1 : 3; }
 __host__ __device__ inline int h_parts(bool bf16) { return bf16 ? 2 : 3; }
 
 // The selected experts that have a slot, in ascending order.
@@ -62,17 +62,17 @@ struct Jobs {
     int expert[MOE_MAX_EXPERTS];
     int slot[MOE_MAX_EXPERTS];
     int count[MOE_MAX_EXPERTS / kWave];
-    int chosen[MOE_MAX_EXPERTS];
+    uint32_t users[MOE_MAX_EXPERTS];   // by expert: the tokens that selected it, a bit each
 };
 
-// From J.chosen (nonzero: selected by some token). Ends with a barrier.
+// From J.users. Ends with a barrier.
 __device__ __forceinline__ void build_jobs(const LayerParams &p, Jobs &J)
 {
     const int e = threadIdx.x, lane = e & 63;
     int slot = -1;
     uint64_t m = 0;
     if (e < MOE_MAX_EXPERTS) {
-        if (e < p.n && J.chosen[e]) {
+        if (e < p.n && J.users[e]) {
             slot = p.slotmap ? p.slotmap[e] : e;
             if (slot >= p.nslots) slot = -1;
         }
@@ -92,57 +92,91 @@ __device__ __forceinline__ void build_jobs(const LayerParams &p, Jobs &J)
     __syncthreads();
 }
 
-// Logits: wave i of the grid takes expert i / T and token i % T.
-__global__ __launch_bounds__(256) void k_layer_logits(LayerParams p)
+// Blocks of the first `logit_blocks`: logits. A wave sums a `split`-th of an (expert, token) row; the
+// work group adds up (four waves: 4 / split rows). Row i is expert i / T and token i % T. The other
+// blocks: x as columns, 8 values of a token and part per thread; and the row counts cleared.
+__global__ __launch_bounds__(256) void k_layer_prepare(LayerParams p, int split, int logit_blocks)
 {
-    const int lane = threadIdx.x & 63;
-    const int i = blockIdx.x * 4 + (threadIdx.x >> 6);
-    if (i >= p.n * p.T) return;
-    const int e = i / p.T, t = i - e * p.T;
-    const float4 *w = reinterpret_cast<const float4 *>(p.wr + (size_t)e * p.d);
-    double acc = 0.0;
-    const int nq = p.d >> 2;
-    auto dot = [&](const float4 a, const float4 b) {
-        acc = fma((double)a.x, (double)b.x, acc);
-        acc = fma((double)a.y, (double)b.y, acc);
-        acc = fma((double)a.z, (double)b.z, acc);
-        acc = fma((double)a.w, (double)b.w, acc);
-    };
-    if (p.bf16) {
-        const uint2 *x = reinterpret_cast<const uint2 *>(static_cast<const uint16_t *>(p.x) + (size_t)t * p.d);
-#pragma unroll 4
-        for (int c = lane; c < nq; c += kWave) {
-            const uint2 v = x[c];
-            dot(w[c], make_float4(__uint_as_float(v.x << 16), __uint_as_float(v.x & 0xffff0000u),
-                                  __uint_as_float(v.y << 16), __uint_as_float(v.y & 0xffff0000u)));
+    __shared__ double part[4];
+    if ((int)blockIdx.x >= logit_blocks) {
+        const int i = (blockIdx.x - logit_blocks) * 256 + threadIdx.x;
+        const int parts = x_parts(p.bf16), cols = p.T * parts;
+        if (i < (p.d + kRows - 1) / kRows) p.counts[i] = 0;
+        if (i >= chunks_of(p.d) * (kChunk / 8) * cols) return;
+        const int c = i % cols, k = i / cols * 8, q = c / p.T, t = c - q * p.T;
+        uint4 o = make_uint4(0, 0, 0, 0);
+        if (k < p.d && p.bf16) {
+            o = *reinterpret_cast<const uint4 *>(static_cast<const uint16_t *>(p.x) + (size_t)t * p.d + k);
+        } else if (k < p.d) {
+            const float *v = static_cast<const float *>(p.x) + (size_t)t * p.d + k;
+            uint32_t u[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) u[j] = part_of<3>(v[2 * j], q) | ((uint32_t)part_of<3>(v[2 * j + 1], q) << 16);
+            o = make_uint4(u[0], u[1], u[2], u[3]);
         }
-    } else {
-        const float4 *x = reinterpret_cast<const float4 *>(static_cast<const float *>(p.x) + (size_t)t * p.d);
-#pragma unroll 4
-        for (int c = lane; c < nq; c += kWave) dot(w[c], x[c]);
+        *reinterpret_cast<uint4 *>(p.xc + (size_t)i * 16) = o;
+        return;
+    }
+    const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6;
+    const int i = blockIdx.x * (4 / split) + wv / split;
+    double acc = 0.0;
+    const int e = i / p.T, t = i - e * p.T;
+    if (i < p.n * p.T) {
+        const float4 *w = reinterpret_cast<const float4 *>(p.wr + (size_t)e * p.d);
+        const int nq = p.d >> 2, step = split * kWave;
+        auto dot = [&](const float4 a, const float4 b) {
+            acc = fma((double)a.x, (double)b.x, acc);
+            acc = fma((double)a.y, (double)b.y, acc);
+            acc = fma((double)a.z, (double)b.z, acc);
+            acc = fma((double)a.w, (double)b.w, acc);
+        };
+        const int c0 = (wv % split) * kWave + lane;
+        if (p.bf16) {
+            const uint2 *x = reinterpret_cast<const uint2 *>(static_cast<const uint16_t *>(p.x) + (size_t)t * p.d);
+#pragma unroll 8
+            for (int c = c0; c < nq; c += step) {
+                const uint2 v = x[c];
+                dot(w[c], make_float4(__uint_as_float(v.x << 16), __uint_as_float(v.x & 0xffff0000u),
+                                      __uint_as_float(v.y << 16), __uint_as_float(v.y & 0xffff0000u)));
+            }
+        } else {
+            const float4 *x = reinterpret_cast<const float4 *>(static_cast<const float *>(p.x) + (size_t)t * p.d);
+#pragma unroll 8
+            for (int c = c0; c < nq; c += step) dot(w[c], x[c]);
+        }
     }
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) acc += __shfl_xor(acc, o, kWave);
-    if (lane == 0) p.logits[(size_t)t * p.n + e] = acc;
+    if (lane == 0) part[wv] = acc;
+    __syncthreads();
+    if (lane == 0 && wv % split == 0 && i < p.n * p.T) {
+        for (int j = 1; j < split; ++j) acc += part[wv + j];
+        p.logits[(size_t)t * p.n + e] = acc;
+    }
 }
 
+// The logits in LDS (NaN counts as -infinity), and no expert selected yet.
+__device__ __forceinline__ void load_logits(const LayerParams &p, double *lg, Jobs &J)
+{
+    for (int i = threadIdx.x; i < p.T * p.n; i += kThreads) {
+        const double v = p.logits[i];
+        lg[i] = v != v ? -INFINITY : v;
+    }
+    if (threadIdx.x < MOE_MAX_EXPERTS) J.users[threadIdx.x] = 0;
+}
 // The top k of every token: sel[t * k + r] = expert of rank r, w its gate weight, J the jobs.
-// An expert's rank is the number of logits before its own (larger, or equal with a lower id; NaN
-// counts as -infinity). lg: room for T * n + T * k doubles.
+// An expert's rank is the number of logits before its own (larger, or equal with a lower id).
+// lg: the logits, and behind them room for T * k doubles.
 __device__ __forceinline__ void select(const LayerParams &p, double *lg, int *sel, float *w, Jobs &J)
 {
     const int tid = threadIdx.x, nl = p.T * p.n, ns = p.T * p.k;
     double *top = lg + nl;
-    for (int i = tid; i < nl; i += kThreads) {
-        const double v = p.logits[i];
-        lg[i] = v != v ? -INFINITY : v;
-    }
-    if (tid < MOE_MAX_EXPERTS) J.chosen[tid] = 0;
     __syncthreads();
     for (int i = tid; i < nl; i += kThreads) {
         const int t = i / p.n, e = i - t * p.n;
         const double *row = lg + t * p.n, v = row[e];
         int rank = 0;
+#pragma unroll 8
         for (int j = 0; j < p.n; ++j) {
             const double o = row[j];
             rank += (o > v || (o == v && j < e)) ? 1 : 0;
@@ -150,7 +184,7 @@ __device__ __forceinline__ void select(const LayerParams &p, double *lg, int *se
         if (rank < p.k) {
             sel[t * p.k + rank] = e;
             top[t * p.k + rank] = v;
-            J.chosen[e] = 1;
+            atomicOr(&J.users[e], 1u << t);
         }
     }
     __syncthreads();
@@ -168,112 +202,115 @@ __device__ __forceinline__ void select(const LayerParams &p, double *lg, int *se
     build_jobs(p, J);
 }
 
-// Fragments of the hidden values: of a job's K step (32 values), column block by column block,
-// lane by lane, the 8 values of the lane. The shared expert's come first.
-__host__ __device__ inline int k_steps(int f) { return (f + kChunk - 1) / kChunk * 2; }
-__device__ __forceinline__ size_t h_steps(const LayerParams &p, int job)   // K steps before the job's; -1: shared
+// Columns of the hidden values before a job's (bytes); job -1: the shared expert.
+__device__ __forceinline__ size_t h_offset(const LayerParams &p, int job)
 {
-    return job < 0 ? 0 : (size_t)(p.shared ? k_steps(p.fs) : 0) + (size_t)job * k_steps(p.f);
+    if (job < 0) return 0;
+    const size_t chunks = (size_t)(p.shared ? chunks_of(p.fs) : 0) + (size_t)job * chunks_of(p.f);
+    return chunks * (kChunk / 8) * p.T * h_parts(p.bf16) * 16;
 }
 
+// Gate/up items: blocks of 8 rows of W1 and the same of W3, the shared expert's first, then the jobs'.
+// Work groups take them in turn.
 struct GateUpSrc {
-    const uint8_t *base0, *base1;
-    size_t half;
-    int c0, cnt;
     const LayerParams &p;
     const Jobs &J;
-    int it, step, total, rbs, rbf;   // next item, items of the layer, row blocks of the shared and of a routed expert
-    template <class R>
-    __device__ __forceinline__ bool next(R &)
+    int it, step, shared;        // the next item; work groups; blocks of the shared expert
+    int total;                   // items (to begin with, the shared expert's)
+    Rows r;                      // bytes, lane_row, c0, cnt are the same for all
+    int cnt;
+    __device__ __forceinline__ Rows next()
     {
-        if (it >= total || cnt == 0) return false;
-        const bool sh = it < rbs;
-        const int job = sh ? 0 : (it - rbs) / rbf, rb = sh ? it : it - rbs - job * rbf;
-        const int f = sh ? p.fs : p.f;
-        const uint8_t *slab = sh ? p.shared : p.pool + (uint64_t)J.slot[job] * p.slab_stride;
-        const size_t K2 = (size_t)p.d * 2;
-        base0 = slab + (size_t)rb * kRows * K2;
-        base1 = base0 + (size_t)f * K2;
-        half = rb * kRows + 8 < f ? 8 * K2 : 0;   // the last block may have 8 rows
-        it += step;
-        return true;
+        r.cnt = it < total ? cnt : 0;
+        if (it < total) {
+            const int rbf = p.f / 8, job = it < shared ? 0 : (it - shared) / rbf;
+            const int rb = it < shared ? it : it - shared - job * rbf, f = it < shared ? p.fs : p.f;
+            r.base = (it < shared ? p.shared : p.pool + (uint64_t)J.slot[job] * p.slab_stride) + (size_t)rb * 16 * p.d;
+            r.half = (size_t)2 * f * p.d;   // from W1 to W3
+            it += step;
+        }
+        return r;
     }
 };
 
-// Gate/up: h = g * SiLU(W1 x) * (W3 x), for every job, row and token. NB = column blocks of x.
+// Tokens that rows of S chunks per wave can come with, at most.
+constexpr int most_tokens(int S) { return S == 1 ? kMaxTok : MOE_LAYER_MAX_VALUES / ((S - 1) * kWaves * kChunk) < kMaxTok ? MOE_LAYER_MAX_VALUES / ((S - 1) * kWaves * kChunk) : kMaxTok; }
+
+// Gate/up: h = g * SiLU(W1 x) * (W3 x), for every job, row and token. The A operand's first 8 rows are
+// W1's, the others W3's. NB = column blocks of x.
 template <int S, int NB>
 __global__ __launch_bounds__(kThreads) void k_layer_gate_up(LayerParams p)
 {
-    constexpr int RS = NB == 1 ? 8 : 6;
-    constexpr int kRing = kWaves * RS * kStageBytes;
-    __shared__ __align__(1024) uint8_t lds[kRing + kWaves * 2 * NB * 1024];
+    constexpr bool STK = NB == 3;
+    constexpr int AB = STK ? 1 : NB;
+    using Stream_t = Stream<S, GateUpSrc>;
+    using Sums_t = Sums<AB>;
+    __shared__ __align__(1024) uint8_t lds[kWaves * Stream_t::kBytes];
+    constexpr size_t kLogits = sizeof(double) * most_tokens(S) * (MOE_MAX_EXPERTS + MOE_MAX_TOPK_INTERNAL);
+    __shared__ __align__(16) uint8_t shared_room[sizeof(Sums_t) > kLogits ? sizeof(Sums_t) : kLogits];   // the logits, then the sums
+    Sums_t &sums = *reinterpret_cast<Sums_t *>(shared_room);
+    double *lg = reinterpret_cast<double *>(shared_room);
     __shared__ Jobs J;
     __shared__ int sel[kMaxSel];
     __shared__ float gate[kMaxSel];
-    const int tid = threadIdx.x, lane = tid & 63, wv = __builtin_amdgcn_readfirstlane(tid >> 6);
-    static_assert((kMaxTok * MOE_MAX_EXPERTS + kMaxSel) * sizeof(double) <= kRing, "the logits fit the ring");
-    select(p, reinterpret_cast<double *>(lds), sel, gate, J);
+    const int tid = threadIdx.x, wv = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int xcols = p.T * x_parts(p.bf16), shared = p.shared ? p.fs / 8 : 0;
+    GateUpSrc src{p, J, (int)blockIdx.x, (int)gridDim.x, shared, shared, {}, 0};
+    part_chunks(chunks_of(p.d), wv, kWaves, src.r.c0, src.cnt);
+    src.r.bytes = p.d * 2;
+    src.r.lane_row = lane_row_of(src.r.bytes);
+    const int cnt = src.cnt;
+    bf16x8_t bx[S][2][NB];
+    load_columns<S, NB, STK>(p.xc + (size_t)src.r.c0 * (kChunk / 8) * xcols * 16, xcols, p.T, cnt, bx);
+    load_logits(p, lg, J);
+    settle(bx);
+    // Where the shared expert fills the ring, it does so while the routing is worked out. (The items
+    // that start() looks at are all its own.)
+    Stream_t st;
+    const bool early = shared > (Stream_t::RS / S + 2) * (int)gridDim.x;
+    if (early) st.start(src, lds + wv * Stream_t::kBytes, p.xc);
+    select(p, lg, sel, gate, J);
     if (blockIdx.x == 0 && tid < p.T * p.k) {
         p.idx[tid] = sel[tid];
         p.w[tid] = gate[tid];
     }
-    const int rbs = p.shared ? (p.fs + kRows - 1) / kRows : 0, rbf = (p.f + kRows - 1) / kRows;
-    const int total = rbs + __builtin_amdgcn_readfirstlane(J.n) * rbf;
-    GateUpSrc src{nullptr, nullptr, 0, 0, 0, p, J, (int)blockIdx.x, (int)gridDim.x, total, rbs, rbf};
-    part_chunks((p.d + kChunk - 1) / kChunk, wv, kWaves, src.c0, src.cnt);
-    Stream<S, 2, NB, RS, GateUpSrc> st;
-    st.ring.row_bytes((int64_t)p.d * 2);
-    st.start(src, lds + wv * RS * kStageBytes);
-    bf16x8_t bx[S][2][NB];
-    const int parts = p.bf16 ? 1 : 3;
-#pragma unroll
-    for (int nb = 0; nb < NB; ++nb) {
-        const int c = nb * 16 + (lane & 15), part = c / p.T, t = c - part * p.T;
-#pragma unroll
-        for (int s = 0; s < S; ++s)
-#pragma unroll
-            for (int kb = 0; kb < 2; ++kb) {
-                const int k = (src.c0 + s) * kChunk + kb * 32 + (lane >> 4) * 8;
-                bx[s][kb][nb] = s < src.cnt && k < p.d && part < parts ? load_part(p.x, p.bf16, (size_t)t * p.d + k, part)
-                                                                       : no_tokens();
-            }
-    }
-    float *red = reinterpret_cast<float *>(lds + kRing);
-    const int nb2 = (p.cols + 15) >> 4, hp = h_parts(p.bf16);
-    for (int it = blockIdx.x; it < total; it += gridDim.x) {
-        floatx4_t acc[2][NB];
-        st.item(src, bx, src.cnt, acc);
-        lds_barrier();                             // the sums before are read
-        put_sums(red, wv, acc);
-        lds_barrier();
-        const bool sh = it < rbs;
-        const int job = sh ? -1 : (it - rbs) / rbf, rb = sh ? it : it - rbs - job * rbf;
-        const int row = tid & 15, t = tid >> 4, i = rb * kRows + row;
-        if (t < p.T && i < (sh ? p.fs : p.f)) {
-            float wt = sh ? 1.f : 0.f;
-            bool mine = sh;
+    const int rbf = p.f / 8, total = shared + __builtin_amdgcn_readfirstlane(J.n) * rbf;
+    src.total = total;
+    if (!early) st.start(src, lds + wv * Stream_t::kBytes, p.xc);
+    const int parts = x_parts(p.bf16), hp = h_parts(p.bf16), hcols = p.T * hp;
+    for (int it = blockIdx.x, n = 0; it < total; it += gridDim.x, ++n) {
+        floatx4_t acc[AB];
+        clear(acc);
+        multiply<S, NB, STK>(st, bx, cnt, acc);
+        st.advance(src);
+        const int out = sums.exchange(n, p.T * 8, acc);
+        if (out < 0) continue;
+        const int row = out & 7, t = out >> 3;
+        if (t < p.T) {
+            const bool sh = it < shared;
+            const int job = sh ? -1 : (it - shared) / rbf, rb = sh ? it : it - shared - job * rbf;
+            const float g = sums.template token<STK>(n, row, t, p.T, parts), u = sums.template token<STK>(n, row + 8, t, p.T, parts);
+            float wt = 1.f;
+            bool mine = true;
             if (!sh) {
                 const int e = J.expert[job];
-                for (int r = 0; r < p.k; ++r)
-                    if (sel[t * p.k + r] == e) {
-                        wt = gate[t * p.k + r];
-                        mine = true;
-                    }
-            }
-            float g = 0.f, u = 0.f;
-            for (int q = 0; q < parts; ++q) {
-                g += get_sum<2, NB>(red, 0, row, q * p.T + t);
-                u += get_sum<2, NB>(red, 1, row, q * p.T + t);
+                mine = J.users[e] >> t & 1;
+                for (int r = 0; r < p.k; ++r) wt = sel[t * p.k + r] == e ? gate[t * p.k + r] : wt;
             }
             const float hv = mine ? wt * (g / (1.0f + expf(-g)) * u) : 0.f;
-            const size_t step = h_steps(p, job) + (i >> 5);
+            uint8_t *h = p.h + h_offset(p, job);
+            const int f = sh ? p.fs : p.f;
             for (int q = 0; q < hp; ++q) {
-                const int c = q * p.T + t;
-                uint8_t *dst = p.h + ((step * nb2 + (c >> 4)) * kWave + ((i & 31) >> 3) * 16 + (c & 15)) * 16 + (i & 7) * 2;
-                *reinterpret_cast<uint16_t *>(dst) = hp == 3 ? part_of<3>(hv, q) : part_of<2>(hv, q);
+                *reinterpret_cast<uint16_t *>(h + column_at((size_t)rb * 8 + row, hcols, q * p.T + t)) =
+                    hp == 3 ? part_of<3>(hv, q) : part_of<2>(hv, q);
+                // the last block clears the rest of the last chunk
+                if (rb == f / 8 - 1)
+                    for (int k = f + row; k < chunks_of(f) * kChunk; k += 8)
+                        *reinterpret_cast<uint16_t *>(h + column_at(k, hcols, q * p.T + t)) = 0;
             }
         }
     }
+    st.end();
 }
 
 // A wave's unit of the hidden columns: unit u of the layer (the shared expert's first).
@@ -285,152 +322,122 @@ __device__ __forceinline__ Unit unit_of(const LayerParams &p, int u, int us, int
     Unit r{-1, p.fs, 0, 0};
     if (u >= units) return r;
     if (u < us) {
-        part_chunks((p.fs + kChunk - 1) / kChunk, u, us, r.c0, r.cnt);
+        part_chunks(chunks_of(p.fs), u, us, r.c0, r.cnt);
     } else {
         r.job = (u - us) / uf;
         r.f = p.f;
-        part_chunks((p.f + kChunk - 1) / kChunk, u - us - r.job * uf, uf, r.c0, r.cnt);
+        part_chunks(chunks_of(p.f), u - us - r.job * uf, uf, r.c0, r.cnt);
     }
     return r;
 }
+__device__ __forceinline__ const uint8_t *h_of(const LayerParams &p, const Unit &u)
+{
+    return p.h + h_offset(p, u.job) + (size_t)u.c0 * (kChunk / 8) * p.T * h_parts(p.bf16) * 16;
+}
 
 struct DownSrc {
-    const uint8_t *base0, *base1;
-    size_t half;
-    int c0, cnt;
     const LayerParams &p;
     const Jobs &J;
-    int wv, it, end, rbs, us, uf, units, group;
+    int wv, it, end, rbs, us, uf, units;
+    int group;               // of the next item; what this wave has in it
     const uint8_t *w2;
-    size_t K2;
-    template <class R>
-    __device__ __forceinline__ bool next(R &ring)
+    Rows r;
+    __device__ __forceinline__ Rows next()
     {
-        for (;;) {
-            if (it >= end) return false;
-            const int g = it / rbs;
-            if (g != group) {
-                group = g;
-                const Unit u = unit_of(p, g * kWaves + wv, us, uf, units);
-                c0 = u.c0;
-                cnt = u.cnt;
-                K2 = (size_t)u.f * 2;
-                const uint8_t *slab = u.job < 0 ? p.shared : p.pool + (uint64_t)J.slot[u.job] * p.slab_stride;
-                w2 = slab + (size_t)2 * u.f * p.d * 2;
-                ring.row_bytes((int64_t)K2);
-            }
-            if (cnt) break;
-            it = (g + 1) * rbs;   // nothing for this wave in the group
+        if (it >= end) {
+            r.cnt = 0;
+            return r;
         }
-        const int rb = it - group * rbs;
-        base0 = w2 + (size_t)rb * kRows * K2;
-        half = rb * kRows + 8 < p.d ? 8 * K2 : 0;
-        ++it;
-        return true;
-    }
-};
-
-// Down: the sums of group g (eight units of hidden columns) for 16 rows of W2 and all tokens. A
-// work group takes an equal, contiguous share of the (group, row block) items. kOne: there is
-// one group, whose sums are the layer's output.
-template <int S, int NB, bool kOne>
-__global__ __launch_bounds__(kThreads) void k_layer_down(LayerParams p)
-{
-    constexpr int RS = 8;
-    constexpr int kRing = kWaves * RS * kStageBytes;
-    __shared__ __align__(1024) uint8_t lds[kRing + kWaves * NB * 1024];
-    __shared__ Jobs J;
-    const int tid = threadIdx.x, lane = tid & 63, wv = __builtin_amdgcn_readfirstlane(tid >> 6);
-    if (tid < MOE_MAX_EXPERTS) J.chosen[tid] = 0;
-    __syncthreads();
-    if (tid < p.T * p.k) J.chosen[p.idx[tid]] = 1;
-    __syncthreads();
-    build_jobs(p, J);
-    const int chunks_s = p.shared ? (p.fs + kChunk - 1) / kChunk : 0, chunks_f = (p.f + kChunk - 1) / kChunk;
-    const int us = (chunks_s + S - 1) / S, uf = (chunks_f + S - 1) / S;
-    const int units = us + __builtin_amdgcn_readfirstlane(J.n) * uf;
-    const int rbs = (p.d + kRows - 1) / kRows;
-    const int groups = kOne ? 1 : (units + kWaves - 1) / kWaves;
-    const int64_t total = (int64_t)groups * rbs;
-    const int it0 = (int)(total * blockIdx.x / gridDim.x), it1 = (int)(total * (blockIdx.x + 1) / gridDim.x);
-    DownSrc src{nullptr, nullptr, 0, 0, 0, p, J, wv, it0, it1, rbs, us, uf, units, -1, nullptr, 0};
-    Stream<S, 1, NB, RS, DownSrc> st;
-    st.start(src, lds + wv * RS * kStageBytes);
-    float *red = reinterpret_cast<float *>(lds + kRing);
-    const int parts = h_parts(p.bf16);
-    bf16x8_t bx[S][2][NB];
-    int group = -1;
-    Unit u{};
-    for (int it = it0; it < it1; ++it) {
         const int g = it / rbs, rb = it - g * rbs;
         if (g != group) {
             group = g;
-            u = unit_of(p, g * kWaves + wv, us, uf, units);
-            const size_t step0 = h_steps(p, u.job) + 2 * u.c0;
-#pragma unroll
-            for (int s = 0; s < S; ++s)
-#pragma unroll
-                for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-                    for (int nb = 0; nb < NB; ++nb) {
-                        const int k = (u.c0 + s) * kChunk + kb * 32 + (lane >> 4) * 8;
-                        const bool live = s < u.cnt && k < u.f && nb * 16 + (lane & 15) < p.cols;
-                        bx[s][kb][nb] = live ? *reinterpret_cast<const bf16x8_t *>(
-                                                   p.h + (((step0 + 2 * s + kb) * NB + nb) * kWave + lane) * 16)
-                                             : no_tokens();
-                    }
+            const Unit u = unit_of(p, g * kWaves + wv, us, uf, units);
+            w2 = (u.job < 0 ? p.shared : p.pool + (uint64_t)J.slot[u.job] * p.slab_stride) + (size_t)4 * u.f * p.d;
+            r.bytes = u.f * 2;
+            r.lane_row = lane_row_of(r.bytes);
+            r.c0 = u.c0;
+            r.cnt = u.cnt;
         }
-        floatx4_t acc[1][NB];
-        st.item(src, bx, u.cnt, acc);
-        lds_barrier();
-        put_sums(red, wv, acc);
-        lds_barrier();
-        const int row = tid & 15, t = tid >> 4, i = rb * kRows + row;
-        if (t < p.T && i < p.d) {
-            float v = 0.f;
-            for (int q = 0; q < parts; ++q) v += get_sum<1, NB>(red, 0, row, q * p.T + t);
-            const size_t at = (size_t)t * p.d + i;
-            if (kOne) {
-                if (p.bf16) {
-                    if (p.y_in) v += static_cast<float>(static_cast<const __bf16 *>(p.y_in)[at]);
-                    static_cast<__bf16 *>(p.y)[at] = static_cast<__bf16>(v);
-                } else {
-                    if (p.y_in) v += static_cast<const float *>(p.y_in)[at];
-                    static_cast<float *>(p.y)[at] = v;
-                }
-            } else {
-                p.partial[(size_t)g * p.T * p.d + at] = v;
-            }
-        }
+        r.base = w2 + (size_t)rb * kRows * r.bytes;
+        r.half = rb * kRows + 8 < p.d ? (size_t)8 * r.bytes : 0;   // the last block may have 8 rows
+        ++it;
+        return r;
     }
-}
+};
 
-// y = y_in + the groups' sums, in order.
-template <int S>
-__global__ __launch_bounds__(256) void k_layer_sum(LayerParams p)
+constexpr int kKeptSums = 4096;   // 16 KiB: 8 tokens of 32 items
+
+// Down: the sums of group g (eight units of hidden columns) for 16 rows of W2 and all tokens. A
+// work group takes an equal, contiguous share of the (group, row block) items. one: there is one
+// group, whose sums are the layer's output.
+template <int S, int NB, bool STK>
+__global__ __launch_bounds__(kThreads) void k_layer_down(LayerParams p, bool one)
 {
+    constexpr int AB = STK ? 1 : NB;
+    using Stream_t = Stream<S, DownSrc>;
+    __shared__ __align__(1024) uint8_t lds[kWaves * Stream_t::kBytes];
+    __shared__ __align__(16) Sums<AB> sums;
     __shared__ Jobs J;
-    const int tid = threadIdx.x;
-    J.chosen[tid] = 0;
+    __shared__ int todo[kThreads];
+    __shared__ float kept[kKeptSums];
+    const int tid = threadIdx.x, wv = __builtin_amdgcn_readfirstlane(tid >> 6);
+    if (tid < MOE_MAX_EXPERTS) J.users[tid] = 0;
     __syncthreads();
-    if (tid < p.T * p.k) J.chosen[p.idx[tid]] = 1;
+    if (tid < p.T * p.k) atomicOr(&J.users[p.idx[tid]], 1u << tid / p.k);
     __syncthreads();
     build_jobs(p, J);
-    const int chunks_s = p.shared ? (p.fs + kChunk - 1) / kChunk : 0, chunks_f = (p.f + kChunk - 1) / kChunk;
-    const int units = (chunks_s + S - 1) / S + J.n * ((chunks_f + S - 1) / S);
-    const int groups = (units + kWaves - 1) / kWaves;
-    const int at = blockIdx.x * 256 + tid, n = p.T * p.d;
-    if (at >= n) return;
-    float v = 0.f;
-#pragma unroll 8
-    for (int g = 0; g < groups; ++g) v += p.partial[(size_t)g * n + at];
-    if (p.bf16) {
-        if (p.y_in) v += static_cast<float>(static_cast<const __bf16 *>(p.y_in)[at]);
-        static_cast<__bf16 *>(p.y)[at] = static_cast<__bf16>(v);
-    } else {
-        if (p.y_in) v += static_cast<const float *>(p.y_in)[at];
-        static_cast<float *>(p.y)[at] = v;
+    const int us = p.shared ? (chunks_of(p.fs) + S - 1) / S : 0, uf = (chunks_of(p.f) + S - 1) / S;
+    const int units = us + __builtin_amdgcn_readfirstlane(J.n) * uf;
+    const int rbs = (p.d + kRows - 1) / kRows;
+    const int groups = one ? 1 : max(1, (units + kWaves - 1) / kWaves);
+    const int64_t total = (int64_t)groups * rbs;
+    const int it0 = (int)(total * blockIdx.x / gridDim.x), it1 = (int)(total * (blockIdx.x + 1) / gridDim.x);
+    const int parts = h_parts(p.bf16), cols = p.T * parts;
+    int group = it0 / rbs;
+    Unit u = unit_of(p, group * kWaves + wv, us, uf, units);
+    bf16x8_t bx[S][2][NB];
+    load_columns<S, NB, STK>(h_of(p, u), cols, p.T, u.cnt, bx);
+    settle(bx);
+    DownSrc src{p, J, wv, it0, it1, rbs, us, uf, units, -1, nullptr, {}};
+    Stream_t st;
+    st.start(src, lds + wv * Stream_t::kBytes, p.xc);
+    auto output = [&](int t, int row, float v) {
+        const size_t at = (size_t)t * p.d + row;
+        if (p.bf16) {
+            if (p.y_in) v += static_cast<float>(static_cast<const __bf16 *>(p.y_in)[at]);
+            static_cast<__bf16 *>(p.y)[at] = static_cast<__bf16>(v);
+        } else {
+            if (p.y_in) v += static_cast<const float *>(p.y_in)[at];
+            static_cast<float *>(p.y)[at] = v;
+        }
+    };
+    const Partials partials{p.partial, p.counts, kept, kKeptSums, groups, rbs, p.d, p.T, it0, it1};
+    for (int it = it0, n = 0; it < it1; ++it, ++n) {
+        const int g = it / rbs;
+        if (g != group) {
+            group = g;
+            u = unit_of(p, g * kWaves + wv, us, uf, units);
+            load_columns<S, NB, STK>(h_of(p, u), cols, p.T, u.cnt, bx);
+            settle(bx);
+        }
+        floatx4_t acc[AB];
+        clear(acc);
+        multiply<S, NB, STK>(st, bx, u.cnt, acc);
+        st.advance(src);
+        // A token takes the sums of its own experts' units. (Its hidden values are zero in the
+        // others, but their weights may be infinite or NaN.)
+        const uint32_t users = u.cnt == 0 ? 0u : u.job < 0 ? ~0u : J.users[J.expert[u.job]];
+        const int out = sums.exchange(n, p.T * kRows, acc, users);
+        if (out < 0) continue;
+        const int row = out & 15, t = out >> 4;
+        if (t < p.T) {
+            const uint32_t mask = sums.tagged(n, t);
+            const float v = sums.template token<STK>(n, row, t, p.T, parts, mask);
+            partials.put(it, t, row, v, output);
+        }
     }
+    st.end();
+    partials.combine(todo, output);
 }
 
 size_t a256(size_t v) { return (v + 255) & ~(size_t)255; }
@@ -438,22 +445,23 @@ int ceil_div(int a, int b) { return (a + b - 1) / b; }
 
 // Sizes that follow from the call's.
 struct LayerPlan {
-    int cols, nb, s, groups;   // of h: columns and their blocks; chunks of a unit; groups at most
-    size_t logits, idx, w, h, partial, bytes;
+    int nb, s, groups;         // column blocks of h; chunks of a unit; groups at most
+    bool stk;                  // h's parts are stacked
+    size_t logits, idx, w, xc, h, partial, counts, bytes;
 };
 
 LayerPlan plan_layer(int T, int d, int f, int n, int k, int fs, bool bf16)
 {
     LayerPlan L{};
-    L.cols = T * h_parts(bf16);
-    L.nb = ceil_div(L.cols, 16);
+    L.nb = column_blocks(h_parts(bf16), T);
+    L.stk = stacked(h_parts(bf16), T);
     const int jobs = std::min(n, T * k);
-    // Units of 512 columns (256 with three column blocks, whose fragments fill the registers),
-    // shorter where eight of them would hold all the columns.
-    const int64_t chunks = (int64_t)jobs * ceil_div(f, kChunk) + ceil_div(fs, kChunk);
-    L.s = L.nb == 3 ? 4 : 8;
-    while (L.s > 1 && chunks <= (int64_t)L.s / 2 * kWaves) L.s /= 2;
-    const int64_t units = (int64_t)jobs * ceil_div(ceil_div(f, kChunk), L.s) + ceil_div(ceil_div(fs, kChunk), L.s);
+    // Units of up to 8 chunks (4 with three column blocks, whose fragments fill the registers) that
+    // an expert's columns divide into evenly, shorter where eight would hold all the columns.
+    const int64_t chunks = (int64_t)jobs * chunks_of(f) + chunks_of(fs);
+    const int most = (int)std::min<int64_t>(L.nb == 3 ? 4 : 8, (chunks + kWaves - 1) / kWaves);
+    L.s = ceil_div(chunks_of(f), ceil_div(chunks_of(f), most));
+    const int64_t units = (int64_t)jobs * ceil_div(chunks_of(f), L.s) + ceil_div(chunks_of(fs), L.s);
     L.groups = (int)((units + kWaves - 1) / kWaves);
     size_t o = 0;
     auto take = [&](size_t b) {
@@ -464,7 +472,9 @@ LayerPlan plan_layer(int T, int d, int f, int n, int k, int fs, bool bf16)
     L.logits = take((size_t)T * n * 8);
     L.idx = take((size_t)T * k * 4);
     L.w = take((size_t)T * k * 4);
-    L.h = take(((size_t)jobs * k_steps(f) + (fs ? k_steps(fs) : 0)) * L.nb * kWave * 16);
+    L.xc = take((size_t)chunks_of(d) * kChunk * T * x_parts(bf16) * 2);
+    L.h = take(((size_t)jobs * chunks_of(f) + (fs ? chunks_of(fs) : 0)) * kChunk * T * h_parts(bf16) * 2);
+    L.counts = take((size_t)ceil_div(d, kRows) * 4);
     L.partial = take(L.groups > 1 ? (size_t)L.groups * T * d * 4 : 0);
     L.bytes = o;
     return L;
@@ -477,16 +487,12 @@ hipError_t launch_gate_up(const LayerParams &p, hipStream_t s)
     return hipGetLastError();
 }
 
-template <int S, int NB>
+template <int S, int NB, bool STK>
 hipError_t launch_down(const LayerParams &p, int groups, hipStream_t s)
 {
     const int rbs = ceil_div(p.d, kRows);
     const dim3 grid((unsigned)std::min<int64_t>(device_cu_count(), (int64_t)groups * rbs));
-    if (groups == 1) hipLaunchKernelGGL((k_layer_down<S, NB, true>), grid, dim3(kThreads), 0, s, p);
-    else hipLaunchKernelGGL((k_layer_down<S, NB, false>), grid, dim3(kThreads), 0, s, p);
-    hipError_t e = hipGetLastError();
-    if (e != hipSuccess || groups == 1) return e;
-    hipLaunchKernelGGL(k_layer_sum<S>, dim3((unsigned)ceil_div(p.T * p.d, 256)), dim3(256), 0, s, p);
+    hipLaunchKernelGGL((k_layer_down<S, NB, STK>), grid, dim3(kThreads), 0, s, p, groups == 1);
     return hipGetLastError();
 }
 
@@ -494,9 +500,13 @@ hipError_t launch_layer(const LayerParams &p, const LayerPlan &L, hipStream_t s)
 {
     (void)hipGetLastError();
     hipError_t e;
-    hipLaunchKernelGGL(k_layer_logits, dim3((unsigned)ceil_div(p.n * p.T, 4)), dim3(256), 0, s, p);
+    // one wave per row where there are enough of them, else four
+    const int split = p.n * p.T <= 4 * device_cu_count() ? 4 : 1;
+    const int logit_blocks = ceil_div(p.n * p.T, 4 / split);
+    const int column_blocks_x = ceil_div(chunks_of(p.d) * (kChunk / 8) * p.T * x_parts(p.bf16), 256);
+    hipLaunchKernelGGL(k_layer_prepare, dim3((unsigned)(logit_blocks + column_blocks_x)), dim3(256), 0, s, p, split, logit_blocks);
     if ((e = hipGetLastError()) != hipSuccess) return e;
-    const int nb1 = ceil_div(p.T * (p.bf16 ? 1 : 3), 16), s1 = ceil_div(ceil_div(p.d, kChunk), kWaves);
+    const int nb1 = column_blocks(x_parts(p.bf16), p.T), s1 = ceil_div(chunks_of(p.d), kWaves);
     // T * d <= MOE_LAYER_MAX_VALUES: 16 chunks a wave with one column block, 11 with two, 6 with three
     switch (nb1 * 100 + s1) {
 #define MOE_GU(NB, S) \
@@ -510,12 +520,13 @@ hipError_t launch_layer(const LayerParams &p, const LayerPlan &L, hipStream_t s)
     default: return hipErrorInvalidValue;
     }
     if (e != hipSuccess) return e;
-    switch (L.nb * 100 + L.s) {
-#define MOE_DN(NB, S) \
-    case NB * 100 + S: return launch_down<S, NB>(p, L.groups, s);
-        MOE_DN(1, 1) MOE_DN(1, 2) MOE_DN(1, 4) MOE_DN(1, 8)
-        MOE_DN(2, 1) MOE_DN(2, 2) MOE_DN(2, 4) MOE_DN(2, 8)
-        MOE_DN(3, 1) MOE_DN(3, 2) MOE_DN(3, 4)
+    switch (L.nb * 100 + L.s * 10 + L.stk) {
+#define MOE_DN(NB, STK, S) \
+    case NB * 100 + S * 10 + STK: return launch_down<S, NB, STK>(p, L.groups, s);
+        MOE_DN(1, 0, 1) MOE_DN(1, 0, 2) MOE_DN(1, 0, 3) MOE_DN(1, 0, 4) MOE_DN(1, 0, 5) MOE_DN(1, 0, 6) MOE_DN(1, 0, 7) MOE_DN(1, 0, 8)
+        MOE_DN(2, 0, 1) MOE_DN(2, 0, 2) MOE_DN(2, 0, 3) MOE_DN(2, 0, 4) MOE_DN(2, 0, 5) MOE_DN(2, 0, 6) MOE_DN(2, 0, 7) MOE_DN(2, 0, 8)
+        MOE_DN(2, 1, 1) MOE_DN(2, 1, 2) MOE_DN(2, 1, 3) MOE_DN(2, 1, 4) MOE_DN(2, 1, 5) MOE_DN(2, 1, 6) MOE_DN(2, 1, 7) MOE_DN(2, 1, 8)
+        MOE_DN(3, 1, 1) MOE_DN(3, 1, 2) MOE_DN(3, 1, 3) MOE_DN(3, 1, 4)
 #undef MOE_DN
     default: return hipErrorInvalidValue;
     }
@@ -582,8 +593,9 @@ int moe_layer_tokens(const moe_tokens_desc *P, const void *x, int T, const void 
     p.logits = reinterpret_cast<double *>(ws + L.logits);
     p.idx = idx ? idx : reinterpret_cast<int32_t *>(ws + L.idx);
     p.w = w ? w : reinterpret_cast<float *>(ws + L.w);
+    p.xc = ws + L.xc;
     p.h = ws + L.h;
-    p.cols = L.cols;
+    p.counts = reinterpret_cast<uint32_t *>(ws + L.counts);
     p.partial = reinterpret_cast<float *>(ws + L.partial);
     p.y_in = y_in;
     p.y = y;

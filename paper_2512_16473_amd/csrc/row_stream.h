@@ -1,15 +1,14 @@
 // A few tokens against long weight rows: the device code that moe_layer_tokens and
 // moe_adapter_project share (HIP device code only).
 //
-// A work group has 8 waves. It takes weight rows 16 at a time; each wave owns a slice of the
-// reduction (a unit: up to S chunks of 64 columns) and multiplies its slice of the 16 rows
-// with the tokens by v_mfma_f32_16x16x32_bf16, the weights as the A operand and the tokens
-// as the B operand, so the matrix cores do per 1 KiB of weights one or a few instructions
-// and the kernel is bound by reading the weights. The tokens' fragments stay in registers
-// for all the rows; the weights go from memory straight to LDS (8 rows by 128 bytes per
-// load instruction) in a ring of stages that belongs to one wave, so that a wave waits for
-// its own loads only and no barrier stands in the stream. The waves' sums of a row block
-// meet in LDS.
+// A work group has 8 waves. It takes weight rows 16 at a time (an item); each wave owns a slice
+// of the reduction (a unit: up to S chunks of 64 columns) and multiplies its slice of the 16 rows
+// with the tokens by v_mfma_f32_16x16x32_bf16, the weights as the A operand and the tokens as the
+// B operand, so the matrix cores do per KiB of weights one or a few instructions and the kernel is
+// bound by reading the weights. The tokens' fragments stay in registers for all the rows; the
+// weights go from memory straight to LDS (8 rows by 128 bytes per load instruction) in a ring of
+// stages that belongs to one wave, so that a wave waits for its own loads only. The waves' sums of
+// an item meet in LDS (Sums), again without a barrier.
 //
 // Reading 2 GiB this way (rows of 8 KiB, nothing multiplied) runs at 6.80 TB/s, and at 6.94
 // where 8 KiB are read of each 28 KiB row; loading the same fragments into registers (16
@@ -39,168 +38,278 @@ typedef float floatx4_t __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(1))) const void global_cvoid;
 typedef __attribute__((address_space(3))) void lds_void;
 
+typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
+
+__device__ __forceinline__ uint32_t lds_address(const void *p) { return (uint32_t)(uintptr_t)(lds_void *)p; }
+
+__host__ __device__ constexpr int chunks_of(int k) { return (k + kChunk - 1) / kChunk; }
+
 template <int N>
 __device__ __forceinline__ void wait_loads()
 {
     asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
 }
-// This wave's LDS accesses are done; then every wave is here. The weight loads stay in flight.
-__device__ __forceinline__ void lds_barrier()
-{
-    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
-}
 
-// Part p of P (1 to 3) of v in bf16: the parts but the last are cut off, the last is rounded to
-// nearest; three hold all 24 bits. Infinities and NaN have no further parts.
+// Part p of P (2 or 3) of v, as a bf16: the parts but the last are cut off after 8 bits, the last is
+// rounded to nearest (three hold all 24 bits, so the third is exact). v - cut(v) is taken as zero
+// where the two are equal, so an infinity has no further parts; a NaN has NaN parts.
 template <int P>
 __device__ __forceinline__ uint16_t part_of(float v, int p)
 {
-    const uint32_t u = __float_as_uint(v);
-    const float r1 = v - __uint_as_float(u & 0xffff0000u);
-    const float r2 = r1 - __uint_as_float(__float_as_uint(r1) & 0xffff0000u);
-    const float part = p == 0 ? v : p == 1 ? r1 : r2;
-    uint32_t bits = __float_as_uint(part) >> 16;
-    if (p == P - 1) bits = __builtin_bit_cast(uint16_t, static_cast<__bf16>(part));
-    if ((u & 0x7f800000u) == 0x7f800000u) bits = p ? 0 : (u >> 16) | ((u & 0xffffu) ? 0x40u : 0u);
-    return (uint16_t)bits;
+    for (int i = 0; i < p; ++i) {
+        const float cut = __uint_as_float(__float_as_uint(v) & 0xffff0000u);
+        v = v == cut ? 0.f : v - cut;
+    }
+    if (P == 2 && p == 1) return __builtin_bit_cast(uint16_t, static_cast<__bf16>(v));
+    return (uint16_t)(__float_as_uint(v) >> 16);
 }
 
-// 8 consecutive activations from element `at` of `x` (bf16 or fp32), part p of each.
-__device__ __forceinline__ bf16x8_t load_part(const void *x, bool bf16, size_t at, int p)
-{
-    if (bf16) return *reinterpret_cast<const bf16x8_t *>(static_cast<const uint16_t *>(x) + at);
-    const float4 *src = reinterpret_cast<const float4 *>(static_cast<const float *>(x) + at);
-    const float4 a = src[0], b = src[1];
-    const float v[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
-    uint32_t o[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) o[i] = part_of<3>(v[2 * i], p) | ((uint32_t)part_of<3>(v[2 * i + 1], p) << 16);
-    return __builtin_bit_cast(bf16x8_t, make_uint4(o[0], o[1], o[2], o[3]));
-}
+// Token values as the B operand reads them ("columns"): [K / 8][cols][8] bf16, K padded with zeros
+// to whole chunks, cols = parts * T, column q * T + t = part q of token t. The operand's 16-column
+// blocks hold them packed (block c / 16, as many as that takes; the sums of a token's parts are
+// added after the waves' sums) or stacked, where packing would take as many blocks as there are
+// parts: block q, column t, and the blocks' products go into one sum.
+__host__ __device__ constexpr bool stacked(int parts, int tn) { return parts > 1 && (parts * tn + 15) / 16 >= parts; }
+__host__ __device__ constexpr int column_blocks(int parts, int tn) { return (parts * tn + 15) / 16; }
+__device__ __forceinline__ size_t column_at(size_t k, int cols, int c) { return ((k >> 3) * cols + c) * 16 + (k & 7) * 2; }
+
 __device__ __forceinline__ bf16x8_t no_tokens() { return __builtin_bit_cast(bf16x8_t, make_uint4(0, 0, 0, 0)); }
 
-// The ring of one wave: weights of its items in order, stage by stage.
-template <int NM, int RS>
-struct Ring {
-    static_assert(RS % NM == 0, "a chunk of NM matrices is NM stages");
-    uint8_t *lds;              // RS stages
-    int slot, rslot;           // next to read, next to fill
-    int lane_row;              // byte offset of this lane's row within 8 rows
-    int piece, lim;            // byte offset of this lane's 16 bytes in a chunk; the last in a row
-
-    __device__ __forceinline__ void init(uint8_t *mine)
-    {
-        const int lane = threadIdx.x & 63;
-        lds = mine;
-        slot = rslot = 0;
-        // lane l's 16 bytes land at slot l % 8 of row l / 8: chunk c of row r sits at c ^ r, so
-        // that the operand reads (16 rows, one chunk per quarter wave) touch all banks evenly
-        piece = ((lane & 7) ^ (lane >> 3)) * 16;
-    }
-    __device__ __forceinline__ void row_bytes(int64_t K2)
-    {
-        lane_row = (int)(((threadIdx.x & 63) >> 3) * K2);
-        lim = (int)K2 - 16;
-    }
-    // Stage of 16 rows from `base` (rows 8 .. 15 from base + half), chunk `c` of the rows.
-    __device__ __forceinline__ void fill(const uint8_t *base, size_t half, int c)
-    {
-        // past a row's end its last piece is read; the token operand is zero there
-        const int o = min(c * (kChunk * 2) + piece, lim);
-        const uint8_t *p = base + (uint32_t)(lane_row + o);
-        uint8_t *to = lds + rslot * kStageBytes;
-        __builtin_amdgcn_global_load_lds((global_cvoid *)p, (lds_void *)to, 16, 0, 2);   // 2: nontemporal
-        __builtin_amdgcn_global_load_lds((global_cvoid *)(p + half), (lds_void *)(to + kStageBytes / 2), 16, 0, 2);
-        rslot = rslot + 1 == RS ? 0 : rslot + 1;
-    }
-    // A operands of the next stage: its two K steps of 32.
-    __device__ __forceinline__ void read(bf16x8_t (&w)[2])
-    {
-        const int lane = threadIdx.x & 63, row = lane & 15;
-        const uint8_t *p = lds + slot * kStageBytes + row * (kChunk * 2);
-#pragma unroll
-        for (int kb = 0; kb < 2; ++kb) w[kb] = *reinterpret_cast<const bf16x8_t *>(p + ((kb * 4 + (lane >> 4)) ^ (row & 7)) * 16);
-        slot = slot + 1 == RS ? 0 : slot + 1;
-    }
-};
-
-// A wave's way through its items: the ring is kept full from `src`, which runs ahead of the
-// sums by the ring's length. Src has base0 (and base1, the second matrix), half, c0, cnt of the item whose stages come
-// next, and next(), which moves on to the wave's next item with cnt > 0 (false: none is left)
-// and sets the ring's row length.
-template <int S, int NM, int NB, int RS, class Src>
-struct Stream {
-    Ring<NM, RS> ring;
-    bool left;                  // another stage is to be filled; then RS stages are on their way
-    int q;                      // of the item in src: chunks times NM matrices
-
-    __device__ __forceinline__ void issue(Src &src)
-    {
-        if (!left) return;
-        ring.fill(NM == 1 || !(q & 1) ? src.base0 : src.base1, src.half, src.c0 + (NM == 1 ? q : q >> 1));
-        if (++q == NM * src.cnt) {
-            q = 0;
-            left = src.next(ring);
-        }
-    }
-    __device__ __forceinline__ void start(Src &src, uint8_t *lds)
-    {
-        ring.init(lds);
-        q = 0;
-        left = src.next(ring);
-        for (int i = 0; i < RS; ++i) issue(src);
-    }
-    // acc[m][nb] = the sums of one item over this wave's cnt chunks
-    __device__ __forceinline__ void item(Src &src, const bf16x8_t (&bx)[S][2][NB], int cnt, floatx4_t (&acc)[NM][NB])
-    {
-#pragma unroll
-        for (int m = 0; m < NM; ++m)
-#pragma unroll
-            for (int nb = 0; nb < NB; ++nb) acc[m][nb] = floatx4_t{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int s = 0; s < S; ++s) {
-            if (s < cnt) {
-                if (left) wait_loads<2 * (RS - NM)>();
-                else wait_loads<0>();
-                bf16x8_t w[NM][2];
-#pragma unroll
-                for (int m = 0; m < NM; ++m) ring.read(w[m]);
-                asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // read before the slots are filled again
-#pragma unroll
-                for (int m = 0; m < NM; ++m) issue(src);
-#pragma unroll
-                for (int m = 0; m < NM; ++m)
-#pragma unroll
-                    for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-                        for (int nb = 0; nb < NB; ++nb)
-                            acc[m][nb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w[m][kb], bx[s][kb][nb], acc[m][nb], 0, 0, 0);
-            }
-        }
-    }
-};
-
-// The sums of a wave in LDS, [m][nb][256]: a lane's four rows of a column side by side.
-template <int NM, int NB>
-__device__ __forceinline__ void put_sums(float *red, int wv, const floatx4_t (&acc)[NM][NB])
+// The fragments of cnt chunks of columns from `src` (the first chunk's first value). All loads of a
+// column block are in flight at once.
+template <int S, int NB, bool STK>
+__device__ __forceinline__ void load_columns(const uint8_t *src, int cols, int tn, int cnt, bf16x8_t (&bx)[S][2][NB])
 {
     const int lane = threadIdx.x & 63;
 #pragma unroll
-    for (int m = 0; m < NM; ++m)
+    for (int nb = 0; nb < NB; ++nb) {
+        const int c = STK ? nb * tn + (lane & 15) : nb * 16 + (lane & 15);
+        const bool live = STK ? (lane & 15) < tn : c < cols;
+        const uint8_t *p = src + ((size_t)(lane >> 4) * cols + c) * 16;
 #pragma unroll
-        for (int nb = 0; nb < NB; ++nb)
-            *reinterpret_cast<floatx4_t *>(red + ((wv * NM + m) * NB + nb) * 256 + lane * 4) = acc[m][nb];
+        for (int s = 0; s < S; ++s) bx[s][0][nb] = bx[s][1][nb] = no_tokens();
+        if (live) {
+#pragma unroll
+            for (int s = 0; s < S; ++s) {
+                if (s < cnt) {
+                    bx[s][0][nb] = *reinterpret_cast<const bf16x8_t *>(p + (size_t)(2 * s) * cols * 64);
+                    bx[s][1][nb] = *reinterpret_cast<const bf16x8_t *>(p + (size_t)(2 * s + 1) * cols * 64);
+                }
+            }
+        }
+    }
 }
-// Sum over the waves, in order, of matrix m's (row, column c).
-template <int NM, int NB>
-__device__ __forceinline__ float get_sum(const float *red, int m, int row, int c)
+
+// The fragments have arrived: to be called before the ring is started, or in an item loop where they
+// are loaded again. (A use of them would otherwise be the compiler's place to wait, in the loop,
+// and there it waits for the ring's loads as well: one-token Mixtral-shaped down 43 -> 67 us.)
+template <int S, int NB>
+__device__ __forceinline__ void settle(bf16x8_t (&bx)[S][2][NB])
 {
-    const float *p = red + (m * NB + (c >> 4)) * 256 + ((row >> 2) * 16 + (c & 15)) * 4 + (row & 3);
-    float v = 0.f;
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w) v += p[w * NM * NB * 256];
-    return v;
+    for (int s = 0; s < S; ++s)
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb) asm volatile("" : "+v"(bx[s][kb][nb]));
 }
+
+// 16 weight rows as a wave reads its slice of them: 8 rows from `base` and 8 from base + half, of
+// `bytes` bytes each, chunks c0 .. c0 + cnt. lane_row: byte offset of this lane's row.
+struct Rows {
+    const uint8_t *base;
+    size_t half;
+    int bytes, lane_row, c0, cnt;
+};
+__device__ __forceinline__ int lane_row_of(int bytes) { return ((threadIdx.x & 63) >> 3) * bytes; }
+
+// Where a lane finds its 16 bytes of a stage: at b0 + o for its row of the first 8, b1 + o for that
+// of the others. Lane l's 16 bytes land at slot l % 8 of row l / 8: chunk c of row r sits at
+// c ^ r, so that the operand reads (16 rows, one chunk per quarter wave) touch all banks evenly.
+struct Place {
+    const uint8_t *b0, *b1;
+    uint32_t o;
+};
+__device__ __forceinline__ int lane_piece() { return (((int)threadIdx.x & 7) ^ (((int)threadIdx.x & 63) >> 3)) * 16; }
+// Stage s of `r` (past a row's end its last 16 bytes are read; the token operand is zero there).
+__device__ __forceinline__ Place place_of(const Rows &r, int s, const uint8_t *hot)
+{
+    const bool real = s < r.cnt;
+    return {real ? r.base : hot, real ? r.base + r.half : hot,
+            real ? (uint32_t)(r.lane_row + min((r.c0 + s) * (kChunk * 2) + lane_piece(), r.bytes - 16)) : 0u};
+}
+
+// Stages of a ring for items of S stages: at most 4 (64 KiB on their way per work group hide the
+// memory's latency: 470 MB read in 71.5 us with 4 stages, 72.0 with 8; the layer's cases took the
+// same time, within 1 %, with 3, 4 and 5), and a whole number of items, or less than one.
+__host__ __device__ constexpr int ring_stages(int S) { return S >= 4 ? 4 : S * (4 / S); }
+
+// A wave's way through its items of S stages. The ring is kept full: with a stage's operands read, its
+// slot takes the stage RS further on, of this item or a later one, which S and RS say at compile
+// time; the item loop has no branch on what is left, and the code that finds the next item stands
+// once, so that the loop is short. Every stage
+// is two loads, always, so that the wait is a constant: stages that an item does not have, and
+// those past the last item, read 16 bytes at `hot` over and over, and are not multiplied.
+// Src: next() gives the wave's next item, whose stages place_of() finds (past the last: none real).
+template <int S, class Src, class Item = Rows>
+struct Stream {
+    static constexpr int RS = ring_stages(S);
+    static constexpr bool kWhole = RS % S == 0;   // the ring holds whole items: RS / S of them
+    static constexpr int kBytes = RS * kStageBytes;
+    uint8_t *lds;
+    const uint8_t *hot;
+    int slot;                   // of the item's first stage
+    Item cur, nxt;              // the item that is multiplied; the one that is loaded next (kWhole: RS / S items on)
+
+    __device__ __forceinline__ void fill(const Item &r, int s, int at)
+    {
+        const Place p = place_of(r, s, hot);
+        uint8_t *to = lds + at * kStageBytes;
+        __builtin_amdgcn_global_load_lds((global_cvoid *)(p.b0 + p.o), (lds_void *)to, 16, 0, 2);   // 2: nontemporal
+        __builtin_amdgcn_global_load_lds((global_cvoid *)(p.b1 + p.o), (lds_void *)(to + kStageBytes / 2), 16, 0, 2);
+    }
+    __device__ __forceinline__ void start(Src &src, uint8_t *ring, const uint8_t *hot_bytes)
+    {
+        lds = ring;
+        hot = hot_bytes;
+        slot = 0;
+        cur = src.next();
+        if constexpr (kWhole) {
+            nxt = cur;
+#pragma unroll 1
+            for (int at = 0; at < RS; at += S) {
+#pragma unroll
+                for (int s = 0; s < S; ++s) fill(nxt, s, at + s);
+                nxt = src.next();
+            }
+        } else {
+#pragma unroll
+            for (int s = 0; s < RS; ++s) fill(cur, s, s);
+            nxt = src.next();
+        }
+    }
+    // A operands of stage s (two K steps of 32) of the current item; its slot is filled again. The wait
+    // for the stage, the reads and the wait for them are one block: were the reads the compiler's, it
+    // would wait for every load to LDS before some of them.
+    __device__ __forceinline__ void take(int s, bf16x8_t (&w)[2])
+    {
+        const int lane = threadIdx.x & 63, row = lane & 15;
+        int at = slot + s;
+        if (at >= RS) at -= RS;
+        if (!kWhole && at >= RS) at -= RS;
+        if (!kWhole && at >= RS) at -= RS;
+        const uint32_t p = lds_address(lds) + at * kStageBytes + row * (kChunk * 2);
+        const uint32_t p0 = p + ((lane >> 4) ^ (row & 7)) * 16, p1 = p + ((4 + (lane >> 4)) ^ (row & 7)) * 16;
+        asm volatile("s_waitcnt vmcnt(%4)\n\tds_read_b128 %0, %2\n\tds_read_b128 %1, %3\n\ts_waitcnt lgkmcnt(0)"
+                     : "=&v"(w[0]), "=&v"(w[1])
+                     : "v"(p0), "v"(p1), "n"(2 * (RS - 1))
+                     : "memory");
+        if (kWhole) fill(nxt, s, at);
+        else if (s + RS < S) fill(cur, s + RS, at);
+        else fill(nxt, s + RS - S, at);
+    }
+    // To be called once an item's S stages are taken.
+    __device__ __forceinline__ void advance(Src &src)
+    {
+        slot = (slot + S) % RS;
+        if (!kWhole) cur = nxt;
+        nxt = src.next();
+    }
+    // No load is on its way to LDS any more.
+    __device__ __forceinline__ void end() { wait_loads<0>(); }
+};
+
+// acc += the products of one item's first SC stages (cnt of them real) with the columns bx. STK: the
+// column blocks' products go into one sum (stacked parts).
+template <int SC, int NB, bool STK, class St>
+__device__ __forceinline__ void multiply(St &st, const bf16x8_t (&bx)[SC][2][NB], int cnt, floatx4_t (&acc)[STK ? 1 : NB])
+{
+#pragma unroll
+    for (int s = 0; s < SC; ++s) {
+        bf16x8_t w[2];
+        st.take(s, w);
+        if (s < cnt) {
+#pragma unroll
+            for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+                for (int nb = 0; nb < NB; ++nb)
+                    acc[STK ? 0 : nb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w[kb], bx[s][kb][nb], acc[STK ? 0 : nb], 0, 0, 0);
+        }
+    }
+}
+template <int AB>
+__device__ __forceinline__ void clear(floatx4_t (&acc)[AB])
+{
+#pragma unroll
+    for (int nb = 0; nb < AB; ++nb) acc[nb] = floatx4_t{0.f, 0.f, 0.f, 0.f};
+}
+
+// Where the waves' sums of an item meet, two items in turn: with one barrier between the sums and
+// their results, the sums before last are read when the next are put. The results of an item (`outs`
+// of them, up to kThreads) are made by as few waves as hold them, other waves from item to item. The
+// loads on their way are not waited for. (Without a barrier, waves counting each other's sums, a
+// wave could be ahead of the others by an item or more; that was slower, 11 tokens through
+// experts of 1048 x 1816 136 instead of 115 us, one Mixtral-shaped token 129 instead of 124.)
+template <int AB>
+struct Sums {
+    // [wave][block][kSums]: a lane's four rows of a column side by side; the four row groups of a
+    // block are 80 floats apart, so that 16 rows of 4 columns read at once touch all banks
+    static constexpr int kSums = 3 * 80 + 64;
+    float sums[2][kWaves][AB][kSums];
+    alignas(16) uint32_t tag[2][kWaves];   // what a wave says about its sums
+
+    // Puts this wave's sums of the work group's n-th item. Returns this thread's result, or -1.
+    __device__ __forceinline__ int exchange(int n, int outs, const floatx4_t (&acc)[AB], uint32_t what = 0)
+    {
+        const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+#pragma unroll
+        for (int nb = 0; nb < AB; ++nb)
+            *reinterpret_cast<floatx4_t *>(&sums[n & 1][wv][nb][(lane >> 4) * 80 + (lane & 15) * 4]) = acc[nb];
+        if (lane == 0) tag[n & 1][wv] = what;
+        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        const int waves = (outs + kWave - 1) / kWave, w = (wv - n * waves) & (kWaves - 1);
+        return w < waves ? w * kWave + lane : -1;
+    }
+    // Bit w: wave w's tag has bit t.
+    __device__ __forceinline__ uint32_t tagged(int n, int t) const
+    {
+        const uint32_t at = lds_address(&tag[n & 1][0]);
+        u32x4_t a, b;
+        asm volatile("ds_read_b128 %0, %2\n\tds_read_b128 %1, %2 offset:16\n\ts_waitcnt lgkmcnt(0)"
+                     : "=&v"(a), "=&v"(b)
+                     : "v"(at)
+                     : "memory");
+        uint32_t m = 0;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) m |= (a[w] >> t & 1) << w | (b[w] >> t & 1) << (w + 4);
+        return m;
+    }
+    // The sum over the waves, in order, of a row for token t of tn (its parts together, where they
+    // are not stacked). mask: the waves that count.
+    template <bool STK>
+    __device__ __forceinline__ float token(int n, int row, int t, int tn, int parts, uint32_t mask = ~0u) const
+    {
+        float s = 0.f;
+        for (int q = 0; q < (STK ? 1 : parts); ++q) {
+            const int c = q * tn + t;
+            const uint32_t at = lds_address(&sums[n & 1][0][c >> 4][(row >> 2) * 80 + (c & 15) * 4 + (row & 3)]);
+            constexpr int kStep = AB * kSums * 4;
+            float x[kWaves], v = 0.f;
+            // one block of reads, as in Stream::take
+            asm volatile("ds_read_b32 %0, %8\n\tds_read_b32 %1, %8 offset:%9\n\tds_read_b32 %2, %8 offset:%10\n\t"
+                         "ds_read_b32 %3, %8 offset:%11\n\tds_read_b32 %4, %8 offset:%12\n\tds_read_b32 %5, %8 offset:%13\n\t"
+                         "ds_read_b32 %6, %8 offset:%14\n\tds_read_b32 %7, %8 offset:%15\n\ts_waitcnt lgkmcnt(0)"
+                         : "=&v"(x[0]), "=&v"(x[1]), "=&v"(x[2]), "=&v"(x[3]), "=&v"(x[4]), "=&v"(x[5]), "=&v"(x[6]), "=&v"(x[7])
+                         : "v"(at), "n"(kStep), "n"(2 * kStep), "n"(3 * kStep), "n"(4 * kStep), "n"(5 * kStep), "n"(6 * kStep),
+                           "n"(7 * kStep)
+                         : "memory");
+#pragma unroll
+            for (int w = 0; w < kWaves; ++w) v += mask >> w & 1 ? x[w] : 0.f;
+            s += v;
+        }
+        return s;
+    }
+};
 
 // Chunk range [c0, c0 + cnt) of part i of n equal parts of C chunks.
 __device__ __forceinline__ void part_chunks(int C, int i, int n, int &c0, int &cnt)
@@ -208,6 +317,77 @@ __device__ __forceinline__ void part_chunks(int C, int i, int n, int &c0, int &c
     c0 = (int)((int64_t)C * i / n);
     cnt = (int)((int64_t)C * (i + 1) / n) - c0;
 }
+
+// Sums that other work groups of the same launch will read: stores and loads at device scope, which
+// pass the XCD's own L2 by. A work group announces its stores by counters once they have completed:
+// then no cache has to be written back, which a release fence would do for the whole L2.
+__device__ __forceinline__ void store_shared(float *p, float v) { __hip_atomic_store(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+__device__ __forceinline__ float load_shared(const float *p) { return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+
+// Work groups take contiguous shares [it0, it1) of (group, 16 rows) items; their sums add up to the
+// output. Each keeps its items' sums in LDS (`room` floats; what does not fit is passed on at once:
+// a load or a store at device scope takes as long as the loads behind it, and a wave's loads wait
+// for it in order, so that storing every item's at once cost the one-token Mixtral-shaped down 1 us
+// an item). At its end, with one group, it passes them to out(t, row, sum); else it stores them
+// to partial [groups][T][rows] and counts its items per row block, and the one that completes a
+// row block's count adds the block's groups, in order, for out. counts: zero before the launch.
+struct Partials {
+    float *partial;
+    uint32_t *counts;
+    float *kept;      // LDS
+    int room;
+    int groups, rbs, rows, T, it0, it1;
+    __device__ __forceinline__ size_t at(int it, int t, int r) const
+    {
+        const int g = it / rbs, rb = it - g * rbs;
+        return ((size_t)g * T + t) * rows + rb * kRows + r;
+    }
+    template <class Out>
+    __device__ __forceinline__ void put(int it, int t, int r, float v, Out out) const
+    {
+        const int64_t i = ((int64_t)(it - it0) * T + t) * kRows + r;
+        const int row = it % rbs * kRows + r;
+        if (i < room) kept[i] = v;
+        else if (row < rows && groups == 1) out(t, row, v);
+        else if (row < rows) store_shared(partial + at(it, t, r), v);
+    }
+    // The whole work group; todo: kThreads ints of LDS.
+    template <class Out>
+    __device__ __forceinline__ void combine(int *todo, Out out) const
+    {
+        __syncthreads();
+        const int per = T * kRows;
+        const int64_t all = (int64_t)(it1 - it0) * per;
+        for (int i = threadIdx.x; i < all && i < room; i += kThreads) {
+            const int it = it0 + i / per, t = i % per / kRows, r = i % kRows, row = it % rbs * kRows + r;
+            if (row < rows && groups == 1) out(t, row, kept[i]);
+            else if (row < rows) store_shared(partial + at(it, t, r), kept[i]);
+        }
+        if (groups == 1) return;
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");   // all waves' stores have completed
+        for (int base = it0; base < it1; base += kThreads) {
+            const int it = base + threadIdx.x;
+            int rb = -1;
+            if (it < it1) {
+                rb = it % rbs;
+                if (__hip_atomic_fetch_add(&counts[rb], 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) != (uint32_t)groups - 1) rb = -1;
+            }
+            todo[threadIdx.x] = rb;
+            __syncthreads();
+            const int n = min(it1 - base, kThreads) * per;
+            for (int i = threadIdx.x; i < n; i += kThreads) {
+                const int b = todo[i / per], t = i % per / kRows, row = b * kRows + i % kRows;
+                if (b < 0 || row >= rows) continue;
+                const float *p = partial + (size_t)t * rows + row;
+                float v = 0.f;
+#pragma unroll 8
+                for (int g = 0; g < groups; ++g) v += load_shared(p + (size_t)g * T * rows);
+                out(t, row, v);
+            }
+            __syncthreads();
+        }
+    }
+};
 
 }  // namespace row_stream
 }  // namespace moe

@@ -110,6 +110,7 @@ def test_decode_batches(T, d, o, r, n, spread, act):
 @pytest.mark.parametrize("T,d,o,r,n,spread", [
     (17, 8, 8, 8, 2, "each"),            # least of everything
     (17, 4096, 264, 16, 30, "each"),     # one block of 32 rows, split over K
+    (40, 2056, 136, 32, 9, "each"),      # 33 to 48 tokens: a shrink block of four column blocks
     (64, 264, 520, 24, 7, "runs"),       # padded K steps
     (97, 1024, 2048, 128, 3, "each"),    # two K steps of ranks
     (160, 576, 776, 64, 5, "runs"),
@@ -171,6 +172,27 @@ def test_in_place_and_a_token_of_nan(T, act):
         z = c.run()
         assert torch.equal(z[keep], y[keep])
         assert not torch.any(torch.isfinite(z[4]))
+
+
+@pytest.mark.parametrize("act", ACTS)
+@pytest.mark.parametrize("T", [9, 200])
+def test_an_adapter_of_nan_reaches_its_own_tokens_only(T, act):
+    torch = torch_cuda()
+    say("adapter of NaN", T, act)
+    c = Case(torch, T + 50, T, 328, 264, 16, 4, act, "each", y_in=True)
+    y = c.run()
+    mine = c.ids == 2
+    assert 0 < int(mine.sum()) < T
+    for name in ("a", "b"):
+        for bad in (float("nan"), float("inf")):
+            was = getattr(c, name)
+            broken = was.clone()
+            broken[2] = bad
+            setattr(c, name, broken)
+            z = c.run()
+            setattr(c, name, was)
+            assert torch.equal(z[~mine], y[~mine])
+            assert not torch.any(torch.isfinite(z[mine]))
 
 
 @pytest.mark.parametrize("T", [8, 100])

@@ -203,6 +203,28 @@ def test_ties_and_a_token_of_nan():
             assert torch.all(torch.isnan(y[2])) and np.all((idx >= 0) & (idx < n))
 
 
+@pytest.mark.parametrize("act", ["float32", "bfloat16"])
+def test_an_expert_of_nan_reaches_its_own_tokens_only(act):
+    torch = torch_cuda()
+    say("layer_tokens NaN expert", act)
+    d, f, n, k, T = 256, 136, 12, 2, 9
+    layer = Layer(torch, 21, d, f, n, k, 72)
+    x = states(torch, 11, T, d, getattr(torch, act))
+    ey, idx, _, cols = layer.expect(x)
+    for part in (0, f * d, 2 * f * d):                   # W1, W3, W2
+        for bad in (float("nan"), float("inf")):
+            e = int(idx[0, 0])
+            keep = layer.pool[e].clone()
+            layer.pool[e, part:part + f * d] = bad
+            y, _, _ = layer.run(x)
+            layer.pool[e] = keep
+            for t in range(T):
+                if e in idx[t]:
+                    assert not torch.any(torch.isfinite(y[t])), t
+                else:
+                    close(layer, y[t:t + 1], ey[t:t + 1], cols[t:t + 1], f"t={t} beside an expert of {bad}")
+
+
 def test_large_and_small_values():
     """Values near the top of the fp32 range stay finite in the products' parts, tiny ones keep
     their precision (the three parts are exact down to 2^-110)."""
