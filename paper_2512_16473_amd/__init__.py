@@ -49,6 +49,11 @@ def _ptr(t):
     return None if t is None else ctypes.c_void_p(t.data_ptr())
 
 
+def _addr(t):
+    """_ptr as a plain number (0 for None)."""
+    return 0 if t is None else t.data_ptr()
+
+
 def _stream(stream):
     import torch
     if stream is None:
@@ -208,27 +213,41 @@ def expert_ffn_tokens(x, slot_pool, n_slots, slots, w, d, f, y, workspace, strea
 def _act_type(t):
     """MOE_F32 or MOE_BF16 for a tensor of activations."""
     import torch
-    kinds = {torch.float32: _abi.F32, torch.bfloat16: _abi.BF16}
-    if t.dtype not in kinds:
-        raise ValueError(f"activations must be float32 or bfloat16, not {t.dtype}")
-    return kinds[t.dtype]
+    if t.dtype == torch.float32:
+        return _abi.F32
+    if t.dtype == torch.bfloat16:
+        return _abi.BF16
+    raise ValueError(f"activations must be float32 or bfloat16, not {t.dtype}")
 
 
 def _want(fn, name, t, shape, dtype, device):
     """A tensor argument as the library reads it: contiguous, of that shape and type, on x's device."""
-    if t is None:
-        return
-    if tuple(t.shape) != tuple(shape) or t.dtype != dtype or t.device != device or not t.is_contiguous():
-        raise ValueError(f"{fn}: {name} must be a contiguous {dtype} tensor of shape {tuple(shape)} on {device}, "
+    if t is not None and not (t.shape == shape and t.dtype is dtype and t.get_device() == device and t.is_contiguous()):
+        raise ValueError(f"{fn}: {name} must be a contiguous {dtype} tensor of shape {tuple(shape)} on GPU {device}, "
                          f"not {t.dtype} {tuple(t.shape)} (strides {t.stride()}) on {t.device}")
 
 
-def _on_device(fn, x):
-    """The library launches on the current device."""
-    import torch
-    if x.device.type != "cuda":
+def _want_bytes(fn, name, t, nbytes, device):
+    if nbytes > 0 and not (t is not None and t.get_device() == device and t.is_contiguous() and t.nbytes >= nbytes):
+        raise ValueError(f"{fn}: {name} must hold {nbytes} contiguous bytes on GPU {device}")
+
+
+def _gpu_of(fn, x):
+    """x's device index (the library launches on the current device: see _on)."""
+    device = x.get_device()
+    if device < 0:
         raise ValueError(f"{fn}: x must be on the GPU, not on {x.device}")
-    return torch.cuda.device(x.device)
+    return device
+
+
+def _on(device, fn, call, *args, stream):
+    """call(*args, stream) with `device` the current one."""
+    import torch
+    if device == torch.cuda.current_device():
+        _check(fn, call(*args, _stream(stream)))
+    else:
+        with torch.cuda.device(device):
+            _check(fn, call(*args, _stream(stream)))
 
 
 def layer_tokens_workspace_bytes(T, d, f, n, k, f_shared=0) -> int:
@@ -244,38 +263,32 @@ def layer_tokens(x, w_router, slot_pool, f, k, y, workspace, n_slots=None, slotm
     idx int32 / w fp32 [T, k] receive the routing if given. Runs on x's device."""
     import torch
     T, d = x.shape
-    n = int(w_router.shape[0])
-    fn, act = "layer_tokens", _act_type(x)
-    n_slots = n if n_slots is None else int(n_slots)
-    _want(fn, "x", x, (T, d), x.dtype, x.device)
-    _want(fn, "y", y, (T, d), x.dtype, x.device)
-    _want(fn, "y_in", y_in, (T, d), x.dtype, x.device)
-    _want(fn, "w_router", w_router, (n, d), torch.float32, x.device)
-    _want(fn, "slotmap", slotmap, (n,), torch.int32, x.device)
-    _want(fn, "idx", idx, (T, k), torch.int32, x.device)
-    _want(fn, "w", w, (T, k), torch.float32, x.device)
-    for name, t, need in (("slot_pool", slot_pool, n_slots * slab_bytes(d, f)),
-                          ("shared", shared, 6 * d * f_shared)):
-        if need > 0 and (t is None or t.device != x.device or not t.is_contiguous()
-                         or t.numel() * t.element_size() < need):
-            raise ValueError(f"{fn}: {name} must hold {need} contiguous bytes on {x.device}")
-    P = TokensDesc(d, f, n, k, f_shared, n_slots, w_router.data_ptr(), None if slot_pool is None else slot_pool.data_ptr(),
-                   None if slotmap is None else slotmap.data_ptr(), None if shared is None else shared.data_ptr())
-    with _on_device(fn, x):
-        _check("moe_layer_tokens", _lib.moe_layer_tokens(
-            ctypes.byref(P), _ptr(x), T, _ptr(y_in), _ptr(y), _ptr(idx), _ptr(w), act, _ptr(workspace),
-            workspace.numel() * workspace.element_size(), _stream(stream)))
+    n = w_router.shape[0]
+    fn, act, dtype = "layer_tokens", _act_type(x), x.dtype
+    device = _gpu_of(fn, x)
+    n_slots = n if n_slots is None else n_slots
+    _want(fn, "x", x, (T, d), dtype, device)
+    _want(fn, "y", y, (T, d), dtype, device)
+    _want(fn, "y_in", y_in, (T, d), dtype, device)
+    _want(fn, "w_router", w_router, (n, d), torch.float32, device)
+    _want(fn, "slotmap", slotmap, (n,), torch.int32, device)
+    _want(fn, "idx", idx, (T, k), torch.int32, device)
+    _want(fn, "w", w, (T, k), torch.float32, device)
+    _want_bytes(fn, "slot_pool", slot_pool, n_slots * ((6 * d * f + 255) // 256 * 256), device)
+    _want_bytes(fn, "shared", shared, 6 * d * f_shared, device)
+    _want_bytes(fn, "workspace", workspace, 1, device)
+    P = TokensDesc(d, f, n, k, f_shared, n_slots, w_router.data_ptr(), _addr(slot_pool), _addr(slotmap), _addr(shared))
+    _on(device, "moe_layer_tokens", _lib.moe_layer_tokens, ctypes.byref(P), x.data_ptr(), T, _addr(y_in), y.data_ptr(),
+        _addr(idx), _addr(w), act, workspace.data_ptr(), workspace.nbytes, stream=stream)
     return y
 
 
 # --------------------------------------------------------------------------- adapters beside a projection
 def _want_rows(fn, name, t, shape, dtype, device):
     """Rows of contiguous values, any row stride."""
-    if t is None:
-        return
-    if tuple(t.shape) != tuple(shape) or t.dtype != dtype or t.device != device or t.stride(1) != 1:
-        raise ValueError(f"{fn}: {name} must be a {dtype} tensor of shape {tuple(shape)} on {device} with contiguous rows, "
-                         f"not {t.dtype} {tuple(t.shape)} (strides {t.stride()}) on {t.device}")
+    if t is not None and not (t.shape == shape and t.dtype is dtype and t.get_device() == device and t.stride(1) == 1):
+        raise ValueError(f"{fn}: {name} must be a {dtype} tensor of shape {tuple(shape)} on GPU {device} with contiguous "
+                         f"rows, not {t.dtype} {tuple(t.shape)} (strides {t.stride()}) on {t.device}")
 
 
 def _row_stride(t):
@@ -295,25 +308,24 @@ def adapter_project(x, w, a, b, adapters, y, workspace, scale=None, y_in=None, s
     fp32 or bf16, rows contiguous; w: cuda bf16 [d_out, d_in] or None; a: bf16 [n, rank, d_in];
     b: bf16 [n, d_out, rank]; adapters: int32 [T]; scale: fp32 [n]. Runs on x's device."""
     import torch
-    fn, act = "adapter_project", _act_type(x)
+    fn, act, dtype = "adapter_project", _act_type(x), x.dtype
+    device = _gpu_of(fn, x)
     T, d_in = x.shape
-    n, rank = int(a.shape[0]), int(a.shape[1])
-    d_out = int(b.shape[1])
-    _want_rows(fn, "x", x, (T, d_in), x.dtype, x.device)
-    _want_rows(fn, "y", y, (T, d_out), x.dtype, x.device)
-    _want_rows(fn, "y_in", y_in, (T, d_out), x.dtype, x.device)
-    _want(fn, "w", w, (d_out, d_in), torch.bfloat16, x.device)
-    _want(fn, "a", a, (n, rank, d_in), torch.bfloat16, x.device)
-    _want(fn, "b", b, (n, d_out, rank), torch.bfloat16, x.device)
-    _want(fn, "adapters", adapters, (T,), torch.int32, x.device)
-    _want(fn, "scale", scale, (n,), torch.float32, x.device)
-    P = AdapterDesc(d_in, d_out, n, rank, None if w is None else w.data_ptr(), a.data_ptr(), b.data_ptr(),
-                    None if scale is None else scale.data_ptr())
-    with _on_device(fn, x):
-        _check("moe_adapter_project", _lib.moe_adapter_project(
-            ctypes.byref(P), _ptr(x), _row_stride(x), T, _ptr(adapters), _ptr(y_in),
-            0 if y_in is None else _row_stride(y_in), _ptr(y), _row_stride(y), act, _ptr(workspace),
-            workspace.numel() * workspace.element_size(), _stream(stream)))
+    n, rank = a.shape[0], a.shape[1]
+    d_out = b.shape[1]
+    _want_rows(fn, "x", x, (T, d_in), dtype, device)
+    _want_rows(fn, "y", y, (T, d_out), dtype, device)
+    _want_rows(fn, "y_in", y_in, (T, d_out), dtype, device)
+    _want(fn, "w", w, (d_out, d_in), torch.bfloat16, device)
+    _want(fn, "a", a, (n, rank, d_in), torch.bfloat16, device)
+    _want(fn, "b", b, (n, d_out, rank), torch.bfloat16, device)
+    _want(fn, "adapters", adapters, (T,), torch.int32, device)
+    _want(fn, "scale", scale, (n,), torch.float32, device)
+    _want_bytes(fn, "workspace", workspace, 1, device)
+    P = AdapterDesc(d_in, d_out, n, rank, _addr(w), a.data_ptr(), b.data_ptr(), _addr(scale))
+    _on(device, "moe_adapter_project", _lib.moe_adapter_project, ctypes.byref(P), x.data_ptr(), _row_stride(x), T,
+        adapters.data_ptr(), _addr(y_in), 0 if y_in is None else _row_stride(y_in), y.data_ptr(), _row_stride(y), act,
+        workspace.data_ptr(), workspace.nbytes, stream=stream)
     return y
 
 

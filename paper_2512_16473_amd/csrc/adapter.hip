@@ -36,7 +36,7 @@ namespace {
 using namespace row_stream;
 
 constexpr int kStreamTokens = 16;    // tokens that the rows kernel takes
-constexpr int kBlockTokens = 64;     // tokens per shrink block of a longer one, at most
+constexpr int kBlockTokens = 128;    // tokens per shrink block of a longer batch, at most
 
 struct AdapterParams {
     const void *x;                // [T][ldx]
@@ -56,8 +56,7 @@ struct AdapterParams {
     uint32_t *counts;             // [row blocks of y]
     int groups;
     // longer
-    int tb;                       // tokens per shrink block
-    int vgroups;                  // K groups of v
+    int tb, vgroups;              // tokens of a shrink block; K groups of v
     float *v;                     // [vgroups][T][r], unscaled
     const uint16_t *xk;           // activations in bf16, their parts side by side: [T][ldk], a part kpart values
     int64_t ldk, kpart;
@@ -302,7 +301,7 @@ __global__ __launch_bounds__(kThreads) void k_adapter_rows(AdapterParams p)
         const int out = sums.exchange(n, p.T * kRows, acc);
         if (out < 0) continue;
         const int row = out & 15, t = out >> 4;
-        if (t < p.T) partials.put(it, t, row, sums.template token<STK>(n, row, t, p.T, parts), output);
+        if (t < p.T) partials.put(n, t, row, sums.template token<STK>(n, row, t, p.T, parts), output);
     }
     st.end();
     partials.combine(todo, output);
@@ -358,92 +357,164 @@ __device__ __forceinline__ int distinct(const AdapterParams &p, int t0, int n, i
     return count;
 }
 
-// The B operand's fragments of chunks [c0, c0 + cnt) of tokens t0 .. t0 + tn, from xk.
-template <int S, int NB, bool STK>
-__device__ __forceinline__ void load_tokens(const AdapterParams &p, int t0, int tn, int c0, int cnt, bf16x8_t (&bx)[S][2][NB])
-{
-    const int lane = threadIdx.x & 63, parts = x_parts(p.bf16);
+// A block of kBlockTokens tokens: the adapter of each, by every wave.
+struct BlockIds {
+    static constexpr int K = kBlockTokens / kWave;
+    int id[K];
+    __device__ __forceinline__ void load(const AdapterParams &p, int t0, int n)
+    {
 #pragma unroll
-    for (int nb = 0; nb < NB; ++nb) {
-        const int c = nb * 16 + (lane & 15), q = STK ? nb : c / tn, t = STK ? lane & 15 : c - q * tn;
-        const uint16_t *src = p.xk + (size_t)(t0 + t) * p.ldk + (size_t)q * p.kpart + c0 * kChunk + (lane >> 4) * 8;
-#pragma unroll
-        for (int s = 0; s < S; ++s) bx[s][0][nb] = bx[s][1][nb] = no_tokens();
-        if (q < parts && t < tn) {
-#pragma unroll
-            for (int s = 0; s < S; ++s) {
-                if (s < cnt) {
-                    bx[s][0][nb] = *reinterpret_cast<const bf16x8_t *>(src + s * kChunk);
-                    bx[s][1][nb] = *reinterpret_cast<const bf16x8_t *>(src + s * kChunk + 32);
-                }
-            }
+        for (int k = 0; k < K; ++k) {
+            const int i = k * kWave + (threadIdx.x & 63);
+            id[k] = i < n ? p.ids[t0 + i] : -1;
         }
     }
-}
-
-struct ShrinkSrc {
-    const AdapterParams &p;
-    const int *list;
-    int it, step, total, rbs, cnt;
-    Rows r;
-    __device__ __forceinline__ Rows next()
+    // Bit b: 16 tokens b of the block hold one of adapter a.
+    __device__ __forceinline__ uint32_t sixteens(int a) const
     {
-        r.cnt = it < total ? cnt : 0;
-        if (it < total) {
-            const int j = it / rbs, rb = it - j * rbs;
-            r.base = p.a + ((size_t)list[j] * p.r + (size_t)rb * kRows) * r.bytes;
-            r.half = rb * kRows + 8 < p.r ? (size_t)8 * r.bytes : 0;   // the last block may have 8 rows
-            it += step;
+        uint32_t m = 0;
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            const uint64_t u = __ballot(id[k] == a);
+#pragma unroll
+            for (int b = 0; b < 4; ++b) m |= (u >> (16 * b) & 0xffff ? 1u : 0u) << (k * 4 + b);
         }
-        return r;
+        return m;
     }
 };
 
-// v of the tokens of block x, K group y; of the block's (adapter, 16 rows) items every gridDim.z-th.
+// The items of a work group: its adapters of the block (every step-th of the list), for each the
+// ranks 64 at a time, the block's 16 tokens at a time that hold it, and the activations' parts.
+struct ShrinkSrc {
+    const AdapterParams &p;
+    const BlockIds &ids;
+    const int32_t *list;
+    int t0, j, step, nlist, halves, parts, cnt;
+    int half, q;              // of the next item
+    uint32_t left;            // its adapter's 16 tokens still to come, this one the lowest
+    Rows r;
+    // Moves to the first item of adapter j on that has any.
+    __device__ __forceinline__ void adapter()
+    {
+        half = q = 0;
+        left = j < nlist ? ids.sixteens(list[j]) : 0;
+    }
+    __device__ __forceinline__ int first_token() const { return min(t0 + __builtin_ctz(left) * 16, p.T - 16); }   // (T > 16)
+    __device__ __forceinline__ Rows next()
+    {
+        r.cnt = j < nlist ? cnt : 0;
+        if (j >= nlist) return r;
+        r.base = reinterpret_cast<const uint8_t *>(p.xk + (size_t)first_token() * p.ldk + (size_t)q * p.kpart);
+        step_on();
+        return r;
+    }
+    __device__ __forceinline__ void step_on()
+    {
+        if (++q < parts) return;
+        q = 0;
+        left &= left - 1;
+        if (left) return;
+        if (++half < halves) {
+            left = ids.sixteens(list[j]);
+            return;
+        }
+        j += step;
+        adapter();
+    }
+};
+
+// v of the tokens of block x, K group y, of the block's adapters every gridDim.z-th. Here the tokens'
+// rows are streamed, 16 at a time, as the A operand, and 16 NB rows of an adapter's A stay in
+// registers as the columns, so that a token's row is read once for each adapter near it. (With the
+// tokens in registers and the A rows streamed past every 64 of them, 4096 tokens of 14336 values and
+// rank 64 took 77 us, XX so.)
 template <int S, int NB>
 __global__ __launch_bounds__(kThreads) void k_adapter_shrink(AdapterParams p)
 {
-    constexpr bool STK = NB == 3;
-    constexpr int AB = STK ? 1 : NB;
     using Stream_t = Stream<S, ShrinkSrc>;
     __shared__ __align__(1024) uint8_t lds[kWaves * Stream_t::kBytes];
-    __shared__ __align__(16) Sums<AB> sums;
+    __shared__ __align__(16) Sums<NB> sums;
     __shared__ int32_t list[kBlockTokens];
-    __shared__ int mine[kBlockTokens], njobs;
-    const int tid = threadIdx.x, wv = __builtin_amdgcn_readfirstlane(tid >> 6);
+    __shared__ int mine[16 + kBlockTokens], nlist;
+    const int tid = threadIdx.x, lane = tid & 63, wv = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int t0 = blockIdx.x * p.tb, tn = min(p.tb, p.T - t0), g = blockIdx.y;
     if (tid < kWave) {
-        mine[tid] = tid < tn ? p.ids[t0 + tid] : -1;
-        const int n = distinct<1>(p, t0, tn, list);
-        if (tid == 0) njobs = n;
+        const int n = distinct<kBlockTokens / kWave>(p, t0, tn, list);
+        if (tid == 0) nlist = n;
     }
+    for (int i = tid; i < 16 + kBlockTokens; i += kThreads) {
+        const int t = t0 - 16 + i;
+        mine[i] = t >= 0 && t < p.T ? p.ids[t] : -1;
+    }
+    BlockIds ids;
+    ids.load(p, t0, tn);
     __syncthreads();
-    const int rbs = (p.r + kRows - 1) / kRows, total = __builtin_amdgcn_readfirstlane(njobs) * rbs;
-    if ((int)blockIdx.z >= total) return;
-    const int units = (chunks_of(p.d) + S - 1) / S;
-    ShrinkSrc src{p, list, (int)blockIdx.z, (int)gridDim.z, total, rbs, 0, {}};
-    unit_chunks(chunks_of(p.d), g * kWaves + wv, units, src.r.c0, src.cnt);
-    src.r.bytes = p.d * 2;
-    src.r.lane_row = lane_row_of(p.d * 2);
-    const int cnt = src.cnt, parts = x_parts(p.bf16);
-    bf16x8_t bx[S][2][NB];
-    load_tokens<S, NB, STK>(p, t0, tn, src.r.c0, cnt, bx);
-    settle(bx);
+    const int adapters = __builtin_amdgcn_readfirstlane(nlist);
+    if ((int)blockIdx.z >= adapters) return;
+    constexpr int kRanks = NB * 16;
+    const int chunks = chunks_of(p.d), units = (chunks + S - 1) / S;
+    int c0, cnt;
+    unit_chunks(chunks, g * kWaves + wv, units, c0, cnt);
+    ShrinkSrc src{p, ids, list, t0, (int)blockIdx.z, (int)gridDim.z, adapters, (p.r + kRanks - 1) / kRanks, x_parts(p.bf16), cnt, 0, 0, 0, {}};
+    src.r.bytes = chunks * kChunk * 2;   // (a row of xk ends with a chunk)
+    src.r.lane_row = lane_row_of((int)(p.ldk * 2));
+    src.r.half = (size_t)p.ldk * 16;
+    src.r.c0 = c0;
+    src.adapter();
+    ShrinkSrc at = src;                  // of the item that is multiplied
     Stream_t st;
     st.start(src, lds + wv * Stream_t::kBytes, reinterpret_cast<const uint8_t *>(p.xk));
-    for (int it = blockIdx.z, n = 0; it < total; it += gridDim.z, ++n) {
-        floatx4_t acc[AB];
+    bf16x8_t bx[S][2][NB];
+    for (int j = -1, half = -1, n = 0; at.j < adapters;) {
+        const int a = list[at.j], h = at.half, t = at.first_token();
+        if (at.j != j || h != half) {    // this adapter's rows of A
+            j = at.j;
+            half = h;
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb) {
+                const int i = h * kRanks + nb * 16 + (lane & 15);
+                const uint16_t *row = reinterpret_cast<const uint16_t *>(p.a) + ((size_t)a * p.r + min(i, p.r - 1)) * p.d;
+#pragma unroll
+                for (int s = 0; s < S; ++s)
+#pragma unroll
+                    for (int kb = 0; kb < 2; ++kb)
+                        bx[s][kb][nb] = *reinterpret_cast<const bf16x8_t *>(row + min((c0 + s) * kChunk + kb * 32 + (lane >> 4) * 8, p.d - 8));
+            }
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+                for (int s = 0; s < S; ++s)
+#pragma unroll
+                    for (int kb = 0; kb < 2; ++kb)
+                        bx[s][kb][nb] = (c0 + s) * kChunk + kb * 32 + (lane >> 4) * 8 < p.d ? bx[s][kb][nb] : no_tokens();
+            settle(bx);
+        }
+        floatx4_t acc[NB];
         clear(acc);
-        multiply<S, NB, STK>(st, bx, cnt, acc);
-        st.advance(src);
-        // (all waves make results: up to 64 tokens of 16 rows)
-        (void)sums.exchange(n, kThreads, acc);
-        const int j = it / rbs, row = tid & 15, i = (it - j * rbs) * kRows + row;
-        for (int t = tid >> 4; t < tn; t += kThreads / kRows)
-            if (i < p.r && mine[t] == list[j])
-                p.v[((size_t)g * p.T + t0 + t) * p.r + i] = sums.template token<STK>(n, row, t, tn, parts);
+        for (int q = 0; q < at.parts; ++q) {
+            multiply<S, NB, false>(st, bx, cnt, acc);
+            st.advance(src);
+            at.step_on();
+        }
+        (void)sums.exchange(n, kThreads, acc);   // (all waves make results)
+        const int row = (wv & 3) * 4 + (lane >> 4);
+#pragma unroll
+        for (int nb = 0; nb < (NB + 1) / 2; ++nb) {
+            const int c = (nb * 2 + (wv >> 2)) * 16 + (lane & 15), i = h * kRanks + c;
+            if (c < kRanks && i < p.r && mine[16 + t + row - t0] == a)
+                p.v[((size_t)g * p.T + t + row) * p.r + i] = sums.template token<false>(n, row, c, 1, 1);
+        }
+        ++n;
     }
     st.end();
+}
+
+// First row of tile mt of m: the ceil(T / 32) blocks of 32 rows spread evenly.
+__host__ __device__ inline int first_row(int T, int m, int mt)
+{
+    const int blocks = (T + 31) / 32;
+    const int b = (int)((int64_t)blocks * mt / m);
+    return b * 32 < T ? b * 32 : T;
 }
 
 struct GemmParams {
@@ -466,9 +537,9 @@ __global__ __launch_bounds__(256) void k_adapter_parts(GemmParams g)
     if ((int)blockIdx.x < lists) {
         const int b = blockIdx.x * 4 + wv;
         if (b >= g.mtiles) return;
-        const int r0 = tile_row(p.T, b);
+        const int r0 = first_row(p.T, g.mtiles, b);
         int32_t *list = g.list + (size_t)b * (kTileM + 1);
-        const int n = distinct<kTileM / kWave>(p, r0, tile_row(p.T, b + 1) - r0, list + 1);
+        const int n = distinct<kTileM / kWave>(p, r0, first_row(p.T, g.mtiles, b + 1) - r0, list + 1);
         if ((threadIdx.x & 63) == 0) list[0] = n;
         return;
     }
@@ -739,7 +810,7 @@ __global__ __launch_bounds__(kThreads) void k_adapter_gemm(GemmParams g)
         }
         t += pl.u0;
         const int mt = t % g.mtiles, nt = t / g.mtiles;
-        const int row0 = tile_row(g.p.T, mt), rows = tile_row(g.p.T, mt + 1) - row0;
+        const int row0 = first_row(g.p.T, g.mtiles, mt), rows = first_row(g.p.T, g.mtiles, mt + 1) - row0;
         const int k0 = (int)((int64_t)g.steps * ks / parts), kn = (int)((int64_t)g.steps * (ks + 1) / parts) - k0;
         const int start = g.mtiles == 1 && kn > 0 ? (int)((unsigned)(nt * kStagger) % (unsigned)kn) : 0;
         const bool ext = ks == parts - 1;
@@ -765,7 +836,7 @@ __global__ __launch_bounds__(256) void k_adapter_tail(GemmParams g)
     const TilePlan pl = g.plan[xcd];
     if (pl.s < 2 || i >= pl.units - pl.full) return;
     const int t = pl.u0 + pl.full + i, mt = t % g.mtiles, nt = t / g.mtiles;
-    const int row0 = tile_row(p.T, mt), rows = tile_row(p.T, mt + 1) - row0;
+    const int row0 = first_row(p.T, g.mtiles, mt), rows = first_row(p.T, g.mtiles, mt + 1) - row0;
     const float *part = g.part + ((size_t)xcd * g.maxparts + (size_t)i * pl.s) * g.prows * kTileN;
     constexpr int kQuads = kTileN / 4;
     for (int c = threadIdx.x; c < kTailRows * kQuads; c += 256) {
@@ -788,27 +859,51 @@ __global__ __launch_bounds__(256) void k_adapter_tail(GemmParams g)
 size_t a256(size_t v) { return (v + 255) & ~(size_t)255; }
 int ceil_div(int64_t a, int64_t b) { return (int)((a + b - 1) / b); }
 
-// A token-block product's shape: column blocks, chunks of a unit (row_stream.h), groups of the
+// The shape of a streamed product (row_stream.h): column blocks, chunks of a unit, groups of the
 // K columns. Units of up to 8 chunks (4 with three column blocks or more, whose fragments fill the
 // registers), as few groups as those make, all units alike.
 struct StreamPlan {
     int nb, s, groups;
 };
-StreamPlan stream_plan(int d, int parts, int tokens)
+StreamPlan stream_plan(int d, int nb)
 {
     StreamPlan q{};
-    q.nb = column_blocks(parts, tokens);
-    if (parts == 1 && q.nb == 3) q.nb = 4;   // (three blocks are stacked parts)
     const int chunks = chunks_of(d);
-    q.groups = ceil_div(ceil_div(chunks, q.nb <= 2 ? 8 : 4), kWaves);
+    q.nb = nb;
+    q.groups = ceil_div(ceil_div(chunks, nb <= 2 ? 8 : 4), kWaves);
     q.s = ceil_div(chunks, q.groups * kWaves);
     return q;
+}
+
+// Shrink: blocks as large as leave some work for most of the chip (a block's adapters' rows of A are
+// read once for it), then units as long. (512 tokens of 4096 values, 8 adapters of rank 32: 35 us in
+// blocks of 128 tokens and units of 8 chunks, 9.5 in blocks of 32 and units of one; 4096 tokens of
+// 14336 values, 16 of rank 64: 67 us in blocks of 128 and units of 4 chunks, some 20 more with blocks of
+// 64 or units of 3.)
+StreamPlan shrink_plan(int T, int d, int r, int *tb)
+{
+    StreamPlan best{};
+    int64_t most = 0;
+    const int nb = r <= 16 ? 1 : r <= 32 ? 2 : 4, chunks = chunks_of(d);
+    for (int t = kBlockTokens; t >= 16; t /= 2)
+        for (int s = nb <= 2 ? 8 : 4; s >= 1; --s) {
+            const int groups = ceil_div(ceil_div(chunks, s), kWaves);
+            if (ceil_div(chunks, groups * kWaves) != s) continue;
+            const int64_t work = (int64_t)ceil_div(T, t) * groups * 3 / 2;   // a block has one and a half adapters, say
+            if (work <= most) continue;
+            most = work;
+            best = StreamPlan{nb, s, groups};
+            *tb = t;
+            if (work >= 160) return best;
+        }
+    return best;
 }
 
 struct AdapterPlan {
     StreamPlan stream;         // of the rows (up to 16 tokens) or of shrink
     bool gemm, copy;
-    int tb, nk, vparts, rq, mtiles, prows, maxparts;
+    int tb, nk, vparts, rq;
+    size_t part_bytes;
     size_t xc, vc, partial, counts;            // up to 16 tokens
     size_t xk, v, vk, list, part, bytes;       // longer
 };
@@ -826,26 +921,22 @@ AdapterPlan plan_adapter(int T, int d, int o, int r, bool bf16)
     L.vparts = v_parts(bf16);
     L.gemm = T > kStreamTokens;
     if (!L.gemm) {
-        L.stream = stream_plan(d, parts, T);
+        L.stream = stream_plan(d, column_blocks(parts, T));
         L.xc = take((size_t)chunks_of(d) * kChunk * T * parts * 2);
         L.vc = take((size_t)L.vparts * T * chunks_of(r) * kChunk * 2);
         L.partial = take(L.stream.groups > 1 ? (size_t)L.stream.groups * T * o * 4 : 0);
         L.counts = take((size_t)ceil_div(o, kRows) * 4);
     } else {
-        // 64 bf16 tokens or 16 fp32 ones to a shrink block: an adapter's rows are read once per block
-        L.tb = std::min(T, bf16 ? kBlockTokens : kStreamTokens);
-        L.stream = stream_plan(d, parts, L.tb);
+        L.stream = shrink_plan(T, d, r, &L.tb);
         L.nk = ceil_div(d, kBK);
         L.copy = !bf16 || d % kBK != 0;   // bf16 rows that end with a K step are read where they are
         L.rq = ceil_div(r, kBK);
-        L.mtiles = tiles_of(T);
-        L.prows = std::min(T, kTileM);
-        L.maxparts = (int)std::min<size_t>(kMaxParts, kPartBytes / ((size_t)kXcds * L.prows * kTileN * 4));
+        L.part_bytes = std::min<size_t>(kPartBytes, (size_t)kXcds * kMaxParts * std::min(T, kTileM) * kTileN * 4);
         L.xk = take(L.copy ? (size_t)T * parts * L.nk * kBK * 2 : 0);
         L.v = take((size_t)L.stream.groups * T * r * 4);
         L.vk = take((size_t)T * L.vparts * L.rq * kBK * 2);
-        L.list = take((size_t)L.mtiles * (kTileM + 1) * 4);
-        L.part = take((size_t)kXcds * L.maxparts * L.prows * kTileN * 4);
+        L.list = take((size_t)ceil_div(T, 32) * (kTileM + 1) * 4);   // tiles of 32 tokens at least
+        L.part = take(L.part_bytes);
     }
     L.bytes = at;
     return L;
@@ -887,15 +978,15 @@ hipError_t launch_decode(AdapterParams p, const AdapterPlan &L, uint8_t *ws, hip
 
 hipError_t launch_shrink(const AdapterParams &p, const AdapterPlan &L, hipStream_t s)
 {
-    const int blocks = ceil_div(p.T, L.tb), items = std::min(L.tb, p.n) * ceil_div(p.r, kRows);
-    // enough work groups for the chip; a block's items are shared out among them
-    const int split = std::max(1, std::min(items, 2 * device_cu_count() / (blocks * L.stream.groups)));
+    // enough work groups for the chip; a block's adapters are shared out among them
+    const int blocks = ceil_div(p.T, L.tb), most = std::min(L.tb, p.n);
+    const int split = std::max(1, std::min(most, 2 * device_cu_count() / (blocks * L.stream.groups)));
     const dim3 grid((unsigned)blocks, (unsigned)L.stream.groups, (unsigned)split);
     switch (L.stream.nb * 100 + L.stream.s) {
 #define MOE_CASE(NB, S) \
     case NB * 100 + S: hipLaunchKernelGGL((k_adapter_shrink<S, NB>), grid, dim3(kThreads), 0, s, p); break;
+        MOE_CASE(1, 1) MOE_CASE(1, 2) MOE_CASE(1, 3) MOE_CASE(1, 4) MOE_CASE(1, 5) MOE_CASE(1, 6) MOE_CASE(1, 7) MOE_CASE(1, 8)
         MOE_CASE(2, 1) MOE_CASE(2, 2) MOE_CASE(2, 3) MOE_CASE(2, 4) MOE_CASE(2, 5) MOE_CASE(2, 6) MOE_CASE(2, 7) MOE_CASE(2, 8)
-        MOE_CASE(3, 1) MOE_CASE(3, 2) MOE_CASE(3, 3) MOE_CASE(3, 4)
         MOE_CASE(4, 1) MOE_CASE(4, 2) MOE_CASE(4, 3) MOE_CASE(4, 4)
 #undef MOE_CASE
     default: return hipErrorInvalidValue;
@@ -903,19 +994,39 @@ hipError_t launch_shrink(const AdapterParams &p, const AdapterPlan &L, hipStream
     return hipGetLastError();
 }
 
-// K parts of the tiles of an XCD's last round: r tiles of `steps` K steps on `slots` work groups. A
-// part costs a few K steps to start, and its sums are written and read again: 2 KiB a row against
-// the (rows + 256) * 128 bytes of a K step.
-int split_of(int r, int steps, int slots, int maxparts, int rows)
+// How the output is cut: mtiles tiles of tokens, and the K parts of a partial round's tiles.
+struct Cut {
+    int mtiles, s;       // s: parts where an XCD has the most tiles left over
+    int64_t cost;
+};
+// What a cut into m tiles of tokens costs, in ns, for the XCD with the most tiles: a K step of a tile
+// takes 250 ns and 6.65 a token (256 tokens: 1.95 us, 128: 1.1), a tile about 3 us beside its steps,
+// and a part's sums are written and read again, 40 ns a token, with another launch at the end.
+// (512 tokens on 4096 x 14336: 97 us with tiles of 128 tokens, 134 with 256; 333 fp32 tokens on 3592 x
+// 2568: 82 with four tiles, 100 with two.)
+Cut cost_of(int T, int m, int ntiles, int steps, int slots, size_t part_bytes)
 {
-    if (r == 0) return 1;
-    int best = 1, least = steps;
-    for (int s = 2; s <= kMaxSplit && s * kMinPartSteps <= steps && r * s <= maxparts; ++s) {
-        const int cost = ceil_div(r * s, slots) * (ceil_div(steps, s) + 2 + 16 * rows / (rows + kTileN)) + 8;
-        if (cost < least) {
-            least = cost;
-            best = s;
+    const int rows = std::min(T, ceil_div(ceil_div(T, 32), m) * 32);
+    const int units = ceil_div((int64_t)m * ntiles, kXcds), full = units / slots, left = units % slots;
+    const int64_t step = 250 + 665 * rows / 100, tile = 3000;
+    const int maxparts = (int)std::min<size_t>(kMaxParts, part_bytes / ((size_t)kXcds * rows * kTileN * 4));
+    Cut c{m, 1, (int64_t)(full + (left > 0)) * (steps * step + tile)};
+    for (int s = 2; s <= kMaxSplit && left > 0 && s * kMinPartSteps <= steps && left * s <= maxparts; ++s) {
+        const int64_t cost = full * (steps * step + tile) + ceil_div(left * s, slots) * (ceil_div(steps, s) * step + tile + 40 * rows) + 8000;
+        if (cost < c.cost) {
+            c.cost = cost;
+            c.s = s;
         }
+    }
+    return c;
+}
+// The cheapest: tiles of 256 tokens down to 32.
+Cut best_cut(int T, int ntiles, int steps, int slots, size_t part_bytes)
+{
+    Cut best = cost_of(T, tiles_of(T), ntiles, steps, slots, part_bytes);
+    for (int h = 7; h >= 1; --h) {
+        const Cut c = cost_of(T, std::max(1, ceil_div(T, 32 * h)), ntiles, steps, slots, part_bytes);
+        if (c.cost < best.cost) best = c;
     }
     return best;
 }
@@ -929,8 +1040,8 @@ hipError_t launch_gemm(AdapterParams p, const AdapterPlan &L, uint8_t *ws, hipSt
     p.xk = L.copy ? xk : static_cast<const uint16_t *>(p.x);
     p.kpart = L.copy ? (int64_t)L.nk * kBK : 0;
     p.ldk = L.copy ? parts * p.kpart : p.ldx;
-    p.tb = L.tb;
     p.v = reinterpret_cast<float *>(ws + L.v);
+    p.tb = L.tb;
     p.vgroups = L.stream.groups;
     if (copy) {
         hipLaunchKernelGGL(k_adapter_cast, dim3((unsigned)ceil_div(parts * p.kpart / 8, 256), (unsigned)p.T), dim3(256), 0, s, p, xk);
@@ -945,20 +1056,21 @@ hipError_t launch_gemm(AdapterParams p, const AdapterPlan &L, uint8_t *ws, hipSt
     g.vparts = L.vparts;
     g.rq = L.rq;
     g.list = reinterpret_cast<int32_t *>(ws + L.list);
-    g.mtiles = L.mtiles;
     g.ntiles = ceil_div(p.o, kTileN);
     g.slots = std::max(1, device_cu_count() / kXcds);
-    g.maxparts = L.maxparts;
-    g.prows = L.prows;
+    const Cut cut = best_cut(p.T, g.ntiles, g.steps, g.slots, L.part_bytes);
+    g.mtiles = cut.mtiles;
+    g.prows = std::min(p.T, ceil_div(ceil_div(p.T, 32), g.mtiles) * 32);
+    g.maxparts = (int)std::min<size_t>(kMaxParts, L.part_bytes / ((size_t)kXcds * g.prows * kTileN * 4));
     g.part = reinterpret_cast<float *>(ws + L.part);
     const int v_blocks = ceil_div((int64_t)p.T * L.rq * kBK, 256);
-    hipLaunchKernelGGL(k_adapter_parts, dim3((unsigned)(ceil_div(L.mtiles, 4) + v_blocks)), dim3(256), 0, s, g);
+    hipLaunchKernelGGL(k_adapter_parts, dim3((unsigned)(ceil_div(g.mtiles, 4) + v_blocks)), dim3(256), 0, s, g);
     if ((e = hipGetLastError()) != hipSuccess) return e;
     const int U = g.mtiles * g.ntiles;
     bool tail = false;
     for (int x = 0; x < kXcds; ++x) {
-        const int left = tile_plan(U, g.slots, x, 1).units % g.slots;
-        g.plan[x] = tile_plan(U, g.slots, x, split_of(left, g.steps, g.slots, g.maxparts, ceil_div(p.T, g.mtiles)));
+        const int left = tile_plan(U, g.slots, x, 1).units % g.slots;   // (an XCD may have a tile less than the others)
+        g.plan[x] = tile_plan(U, g.slots, x, left * cut.s <= g.maxparts ? cut.s : 1);
         tail = tail || (g.plan[x].s > 1 && g.plan[x].units > g.plan[x].full);
     }
     const dim3 grid(kXcds * g.slots);

@@ -164,6 +164,18 @@ __device__ __forceinline__ void load_logits(const LayerParams &p, double *lg, Jo
     }
     if (threadIdx.x < MOE_MAX_EXPERTS) J.users[threadIdx.x] = 0;
 }
+// Gate weight of token t for job j (zero: did not select it), from the selection.
+__device__ __forceinline__ void gate_table(const LayerParams &p, const int *sel, const float *w, const Jobs &J, float *table)
+{
+    for (int i = threadIdx.x; i < J.n * kMaxTok; i += kThreads) {
+        const int j = i / kMaxTok, t = i % kMaxTok;
+        float v = 0.f;
+        if (t < p.T && (J.users[J.expert[j]] >> t & 1))
+            for (int r = 0; r < p.k; ++r) v = sel[t * p.k + r] == J.expert[j] ? w[t * p.k + r] : v;
+        table[i] = v;
+    }
+}
+
 // The top k of every token: sel[t * k + r] = expert of rank r, w its gate weight, J the jobs.
 // An expert's rank is the number of logits before its own (larger, or equal with a lower id).
 // lg: the logits, and behind them room for T * k doubles.
@@ -210,23 +222,31 @@ __device__ __forceinline__ size_t h_offset(const LayerParams &p, int job)
     return chunks * (kChunk / 8) * p.T * h_parts(p.bf16) * 16;
 }
 
-// Gate/up items: blocks of 8 rows of W1 and the same of W3, the shared expert's first, then the jobs'.
-// Work groups take them in turn.
+// Gate/up items: R blocks of 8 rows of W1 and the same of W3 (an expert's last item may have fewer),
+// the shared expert's first, then the jobs'. Work groups take them in turn.
+template <int R>
 struct GateUpSrc {
     const LayerParams &p;
     const Jobs &J;
-    int it, step, shared;        // the next item; work groups; blocks of the shared expert
+    int it, step, shared;        // the next item; work groups; items of the shared expert
     int total;                   // items (to begin with, the shared expert's)
     Rows r;                      // bytes, lane_row, c0, cnt are the same for all
     int cnt;
+    int block, rb, f;            // of the item: the next block, its first one, the expert's width
+    const uint8_t *slab;
     __device__ __forceinline__ Rows next()
     {
-        r.cnt = it < total ? cnt : 0;
-        if (it < total) {
-            const int rbf = p.f / 8, job = it < shared ? 0 : (it - shared) / rbf;
-            const int rb = it < shared ? it : it - shared - job * rbf, f = it < shared ? p.fs : p.f;
-            r.base = (it < shared ? p.shared : p.pool + (uint64_t)J.slot[job] * p.slab_stride) + (size_t)rb * 16 * p.d;
+        if (block == 0 && it < total) {
+            const int items = (p.f / 8 + R - 1) / R, job = it < shared ? 0 : (it - shared) / items;
+            rb = (it < shared ? it : it - shared - job * items) * R;
+            f = it < shared ? p.fs : p.f;
+            slab = it < shared ? p.shared : p.pool + (uint64_t)J.slot[job] * p.slab_stride;
             r.half = (size_t)2 * f * p.d;   // from W1 to W3
+        }
+        r.cnt = it < total && (rb + block) * 8 < f ? cnt : 0;
+        r.base = slab + (size_t)(rb + block) * 16 * p.d;
+        if (++block == R) {
+            block = 0;
             it += step;
         }
         return r;
@@ -238,13 +258,16 @@ constexpr int most_tokens(int S) { return S == 1 ? kMaxTok : MOE_LAYER_MAX_VALUE
 
 // Gate/up: h = g * SiLU(W1 x) * (W3 x), for every job, row and token. The A operand's first 8 rows are
 // W1's, the others W3's. NB = column blocks of x.
+// Blocks of an item: where a block is short, two share a barrier and the latency of its results.
+constexpr int gate_up_blocks(int S, int AB) { return S <= 4 && AB == 1 ? 2 : 1; }
+
 template <int S, int NB>
 __global__ __launch_bounds__(kThreads) void k_layer_gate_up(LayerParams p)
 {
     constexpr bool STK = NB == 3;
-    constexpr int AB = STK ? 1 : NB;
-    using Stream_t = Stream<S, GateUpSrc>;
-    using Sums_t = Sums<AB>;
+    constexpr int AB = STK ? 1 : NB, R = gate_up_blocks(S, AB);
+    using Stream_t = Stream<S, GateUpSrc<R>>;
+    using Sums_t = Sums<R * AB>;
     __shared__ __align__(1024) uint8_t lds[kWaves * Stream_t::kBytes];
     constexpr size_t kLogits = sizeof(double) * most_tokens(S) * (MOE_MAX_EXPERTS + MOE_MAX_TOPK_INTERNAL);
     __shared__ __align__(16) uint8_t shared_room[sizeof(Sums_t) > kLogits ? sizeof(Sums_t) : kLogits];   // the logits, then the sums
@@ -253,9 +276,10 @@ __global__ __launch_bounds__(kThreads) void k_layer_gate_up(LayerParams p)
     __shared__ Jobs J;
     __shared__ int sel[kMaxSel];
     __shared__ float gate[kMaxSel];
+    __shared__ float weights[MOE_MAX_EXPERTS * kMaxTok];
     const int tid = threadIdx.x, wv = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int xcols = p.T * x_parts(p.bf16), shared = p.shared ? p.fs / 8 : 0;
-    GateUpSrc src{p, J, (int)blockIdx.x, (int)gridDim.x, shared, shared, {}, 0};
+    const int xcols = p.T * x_parts(p.bf16), shared = p.shared ? (p.fs / 8 + R - 1) / R : 0;
+    GateUpSrc<R> src{p, J, (int)blockIdx.x, (int)gridDim.x, shared, shared, {}, 0, 0, 0, 0, nullptr};
     part_chunks(chunks_of(p.d), wv, kWaves, src.r.c0, src.cnt);
     src.r.bytes = p.d * 2;
     src.r.lane_row = lane_row_of(src.r.bytes);
@@ -267,48 +291,66 @@ __global__ __launch_bounds__(kThreads) void k_layer_gate_up(LayerParams p)
     // Where the shared expert fills the ring, it does so while the routing is worked out. (The items
     // that start() looks at are all its own.)
     Stream_t st;
-    const bool early = shared > (Stream_t::RS / S + 2) * (int)gridDim.x;
+    const bool early = shared > (Stream_t::RS / S / R + 2) * (int)gridDim.x;
     if (early) st.start(src, lds + wv * Stream_t::kBytes, p.xc);
     select(p, lg, sel, gate, J);
     if (blockIdx.x == 0 && tid < p.T * p.k) {
         p.idx[tid] = sel[tid];
         p.w[tid] = gate[tid];
     }
-    const int rbf = p.f / 8, total = shared + __builtin_amdgcn_readfirstlane(J.n) * rbf;
+    const int items = (p.f / 8 + R - 1) / R, total = shared + __builtin_amdgcn_readfirstlane(J.n) * items;
     src.total = total;
     if (!early) st.start(src, lds + wv * Stream_t::kBytes, p.xc);
+    gate_table(p, sel, gate, J, weights);
+    __syncthreads();
     const int parts = x_parts(p.bf16), hp = h_parts(p.bf16), hcols = p.T * hp;
-    for (int it = blockIdx.x, n = 0; it < total; it += gridDim.x, ++n) {
-        floatx4_t acc[AB];
-        clear(acc);
-        multiply<S, NB, STK>(st, bx, cnt, acc);
-        st.advance(src);
-        const int out = sums.exchange(n, p.T * 8, acc);
-        if (out < 0) continue;
-        const int row = out & 7, t = out >> 3;
-        if (t < p.T) {
-            const bool sh = it < shared;
-            const int job = sh ? -1 : (it - shared) / rbf, rb = sh ? it : it - shared - job * rbf;
-            const float g = sums.template token<STK>(n, row, t, p.T, parts), u = sums.template token<STK>(n, row + 8, t, p.T, parts);
-            float wt = 1.f;
-            bool mine = true;
-            if (!sh) {
-                const int e = J.expert[job];
-                mine = J.users[e] >> t & 1;
-                for (int r = 0; r < p.k; ++r) wt = sel[t * p.k + r] == e ? gate[t * p.k + r] : wt;
-            }
-            const float hv = mine ? wt * (g / (1.0f + expf(-g)) * u) : 0.f;
-            uint8_t *h = p.h + h_offset(p, job);
-            const int f = sh ? p.fs : p.f;
-            for (int q = 0; q < hp; ++q) {
-                *reinterpret_cast<uint16_t *>(h + column_at((size_t)rb * 8 + row, hcols, q * p.T + t)) =
-                    hp == 3 ? part_of<3>(hv, q) : part_of<2>(hv, q);
-                // the last block clears the rest of the last chunk
-                if (rb == f / 8 - 1)
-                    for (int k = f + row; k < chunks_of(f) * kChunk; k += 8)
-                        *reinterpret_cast<uint16_t *>(h + column_at(k, hcols, q * p.T + t)) = 0;
-            }
+    const size_t h_shared = h_offset(p, 0), h_job = h_offset(p, 1) - h_shared;
+    // The results of an item hold up the work group's next barrier, so what can be known before them
+    // is (with divisions, the search for the gate weight and 64-bit addresses among them 11 tokens
+    // through experts of 1048 x 1816 took 116 us, XX without).
+    int job = -1, i = blockIdx.x;   // of the item: its expert (-1: the shared one) and number there
+    auto settle_job = [&]() {
+        if (job < 0 && i >= shared) {
+            i -= shared;
+            job = 0;
         }
+        while (job >= 0 && i >= items) {
+            i -= items;
+            ++job;
+        }
+    };
+    settle_job();
+    for (int it = blockIdx.x, n = 0; it < total; it += gridDim.x, ++n) {
+        floatx4_t all[R * AB];
+#pragma unroll
+        for (int b = 0; b < R; ++b) {
+            floatx4_t acc[AB];
+            clear(acc);
+            multiply<S, NB, STK>(st, bx, cnt, acc);
+            st.advance(src);
+#pragma unroll
+            for (int nb = 0; nb < AB; ++nb) all[b * AB + nb] = acc[nb];
+        }
+        const int out = sums.exchange(n, R * 8 * p.T, all);
+        const int row = out & 7, b = R == 1 ? 0 : out / (8 * p.T), t = (out >> 3) - b * p.T, rb = i * R + b;
+        const int f = job < 0 ? p.fs : p.f;
+        if (out >= 0 && b < R && t < p.T && rb * 8 < f) {
+            const float wt = job < 0 ? 1.f : weights[job * kMaxTok + t];
+            const bool mine = job < 0 || (J.users[J.expert[job]] >> t & 1);
+            const float g = sums.template token<STK>(n, row, t, p.T, parts, ~0u, b * AB), u = sums.template token<STK>(n, row + 8, t, p.T, parts, ~0u, b * AB);
+            const float hv = mine ? wt * (g / (1.0f + expf(-g)) * u) : 0.f;
+            uint8_t *h = p.h + (job < 0 ? 0 : h_shared + job * h_job);   // 8 rows: one step of 8 values of every column
+            const uint32_t at = (rb * hcols + t) * 16 + row * 2, part = p.T * 16;
+            *reinterpret_cast<uint16_t *>(h + at) = hp == 3 ? part_of<3>(hv, 0) : part_of<2>(hv, 0);
+            *reinterpret_cast<uint16_t *>(h + at + part) = hp == 3 ? part_of<3>(hv, 1) : part_of<2>(hv, 1);
+            if (hp == 3) *reinterpret_cast<uint16_t *>(h + at + 2 * part) = part_of<3>(hv, 2);
+            // the last block clears the rest of the last chunk
+            if (rb == f / 8 - 1)
+                for (int k = f / 8; k < chunks_of(f) * (kChunk / 8); ++k)
+                    for (int q = 0; q < hp; ++q) *reinterpret_cast<uint16_t *>(h + (k * hcols + q * p.T + t) * 16 + row * 2) = 0;
+        }
+        i += gridDim.x;
+        settle_job();
     }
     st.end();
 }
@@ -433,7 +475,7 @@ __global__ __launch_bounds__(kThreads) void k_layer_down(LayerParams p, bool one
         if (t < p.T) {
             const uint32_t mask = sums.tagged(n, t);
             const float v = sums.template token<STK>(n, row, t, p.T, parts, mask);
-            partials.put(it, t, row, v, output);
+            partials.put(n, t, row, v, output);
         }
     }
     st.end();

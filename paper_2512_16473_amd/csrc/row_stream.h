@@ -285,14 +285,14 @@ struct Sums {
         return m;
     }
     // The sum over the waves, in order, of a row for token t of tn (its parts together, where they
-    // are not stacked). mask: the waves that count.
+    // are not stacked), in column blocks from `block` on. mask: the waves that count.
     template <bool STK>
-    __device__ __forceinline__ float token(int n, int row, int t, int tn, int parts, uint32_t mask = ~0u) const
+    __device__ __forceinline__ float token(int n, int row, int t, int tn, int parts, uint32_t mask = ~0u, int block = 0) const
     {
         float s = 0.f;
         for (int q = 0; q < (STK ? 1 : parts); ++q) {
             const int c = q * tn + t;
-            const uint32_t at = lds_address(&sums[n & 1][0][c >> 4][(row >> 2) * 80 + (c & 15) * 4 + (row & 3)]);
+            const uint32_t at = lds_address(&sums[n & 1][0][block + (c >> 4)][(row >> 2) * 80 + (c & 15) * 4 + (row & 3)]);
             constexpr int kStep = AB * kSums * 4;
             float x[kWaves], v = 0.f;
             // one block of reads, as in Stream::take
@@ -342,13 +342,16 @@ struct Partials {
         const int g = it / rbs, rb = it - g * rbs;
         return ((size_t)g * T + t) * rows + rb * kRows + r;
     }
+    // Result (t, r) of the share's n-th item.
     template <class Out>
-    __device__ __forceinline__ void put(int it, int t, int r, float v, Out out) const
+    __device__ __forceinline__ void put(int n, int t, int r, float v, Out out) const
     {
-        const int64_t i = ((int64_t)(it - it0) * T + t) * kRows + r;
-        const int row = it % rbs * kRows + r;
-        if (i < room) kept[i] = v;
-        else if (row < rows && groups == 1) out(t, row, v);
+        if ((n + 1) * T * kRows <= room) {   // (n counts a share: far below 2^31 / 256)
+            kept[(n * T + t) * kRows + r] = v;
+            return;
+        }
+        const int it = it0 + n, row = it % rbs * kRows + r;
+        if (row < rows && groups == 1) out(t, row, v);
         else if (row < rows) store_shared(partial + at(it, t, r), v);
     }
     // The whole work group; todo: kThreads ints of LDS.
@@ -356,9 +359,8 @@ struct Partials {
     __device__ __forceinline__ void combine(int *todo, Out out) const
     {
         __syncthreads();
-        const int per = T * kRows;
-        const int64_t all = (int64_t)(it1 - it0) * per;
-        for (int i = threadIdx.x; i < all && i < room; i += kThreads) {
+        const int per = T * kRows, all = min(it1 - it0, room / per) * per;
+        for (int i = threadIdx.x; i < all; i += kThreads) {
             const int it = it0 + i / per, t = i % per / kRows, r = i % kRows, row = it % rbs * kRows + r;
             if (row < rows && groups == 1) out(t, row, kept[i]);
             else if (row < rows) store_shared(partial + at(it, t, r), kept[i]);
