@@ -246,7 +246,6 @@ __global__ __launch_bounds__(kThreads) void k_adapter_rows(AdapterParams p)
     unit_chunks(chunks_of(p.d), group * kWaves + wv, units, c0, cnt);
     bf16x8_t bx[S][2][NB];
     load_columns<S, NB, STK>(p.xc + (size_t)c0 * (kChunk / 8) * cols * 16, cols, p.T, cnt, bx);
-    settle(bx);
     __syncthreads();
     const int adapters = __builtin_amdgcn_readfirstlane(nlist);
     const int mine0 = wv < adapters ? list[wv] : -1, mine1 = wv + kWaves < adapters ? list[wv + kWaves] : -1;
@@ -258,6 +257,7 @@ __global__ __launch_bounds__(kThreads) void k_adapter_rows(AdapterParams p)
     src.r.rc = rc;
     Stream_t st;
     st.start(src, lds + wv * Stream_t::kBytes, p.xc);
+    settle(bx);
     auto output = [&](int t, int row, float s) {
         if (p.y_in) s += load_act(p.y_in, p.bf16, (size_t)t * p.ldyin + row);
         store_act(p.y, p.bf16, (size_t)t * p.ldy + row, s);

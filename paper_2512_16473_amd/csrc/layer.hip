@@ -439,10 +439,10 @@ __global__ __launch_bounds__(kThreads) void k_layer_down(LayerParams p, bool one
     Unit u = unit_of(p, group * kWaves + wv, us, uf, units);
     bf16x8_t bx[S][2][NB];
     load_columns<S, NB, STK>(h_of(p, u), cols, p.T, u.cnt, bx);
-    settle(bx);
     DownSrc src{p, J, wv, it0, it1, rbs, us, uf, units, -1, nullptr, {}};
     Stream_t st;
     st.start(src, lds + wv * Stream_t::kBytes, p.xc);
+    settle(bx);   // (the ring's first loads, a known number, stay on their way)
     auto output = [&](int t, int row, float v) {
         const size_t at = (size_t)t * p.d + row;
         if (p.bf16) {
@@ -498,10 +498,10 @@ LayerPlan plan_layer(int T, int d, int f, int n, int k, int fs, bool bf16)
     L.nb = column_blocks(h_parts(bf16), T);
     L.stk = stacked(h_parts(bf16), T);
     const int jobs = std::min(n, T * k);
-    // Units of up to 8 chunks (4 with three column blocks, whose fragments fill the registers) that
-    // an expert's columns divide into evenly, shorter where eight would hold all the columns.
+    // Units of up to 8 chunks that an expert's columns divide into evenly, shorter where eight would
+    // hold all the columns.
     const int64_t chunks = (int64_t)jobs * chunks_of(f) + chunks_of(fs);
-    const int most = (int)std::min<int64_t>(L.nb == 3 ? 4 : 8, (chunks + kWaves - 1) / kWaves);
+    const int most = (int)std::min<int64_t>(8, (chunks + kWaves - 1) / kWaves);
     L.s = ceil_div(chunks_of(f), ceil_div(chunks_of(f), most));
     const int64_t units = (int64_t)jobs * ceil_div(chunks_of(f), L.s) + ceil_div(chunks_of(fs), L.s);
     L.groups = (int)((units + kWaves - 1) / kWaves);
@@ -568,7 +568,7 @@ hipError_t launch_layer(const LayerParams &p, const LayerPlan &L, hipStream_t s)
         MOE_DN(1, 0, 1) MOE_DN(1, 0, 2) MOE_DN(1, 0, 3) MOE_DN(1, 0, 4) MOE_DN(1, 0, 5) MOE_DN(1, 0, 6) MOE_DN(1, 0, 7) MOE_DN(1, 0, 8)
         MOE_DN(2, 0, 1) MOE_DN(2, 0, 2) MOE_DN(2, 0, 3) MOE_DN(2, 0, 4) MOE_DN(2, 0, 5) MOE_DN(2, 0, 6) MOE_DN(2, 0, 7) MOE_DN(2, 0, 8)
         MOE_DN(2, 1, 1) MOE_DN(2, 1, 2) MOE_DN(2, 1, 3) MOE_DN(2, 1, 4) MOE_DN(2, 1, 5) MOE_DN(2, 1, 6) MOE_DN(2, 1, 7) MOE_DN(2, 1, 8)
-        MOE_DN(3, 1, 1) MOE_DN(3, 1, 2) MOE_DN(3, 1, 3) MOE_DN(3, 1, 4)
+        MOE_DN(3, 1, 1) MOE_DN(3, 1, 2) MOE_DN(3, 1, 3) MOE_DN(3, 1, 4) MOE_DN(3, 1, 5) MOE_DN(3, 1, 6) MOE_DN(3, 1, 7) MOE_DN(3, 1, 8)
 #undef MOE_DN
     default: return hipErrorInvalidValue;
     }

@@ -100,9 +100,9 @@ __device__ __forceinline__ void load_columns(const uint8_t *src, int cols, int t
     }
 }
 
-// The fragments have arrived: to be called before the ring is started, or in an item loop where they
-// are loaded again. (A use of them would otherwise be the compiler's place to wait, in the loop,
-// and there it waits for the ring's loads as well: one-token Mixtral-shaped down 43 -> 67 us.)
+// The fragments have arrived: to be called before the item loop, or in it where they are loaded
+// again. (A use of them would otherwise be the compiler's place to wait, in the loop, and there
+// it waits for the ring's loads as well.)
 template <int S, int NB>
 __device__ __forceinline__ void settle(bf16x8_t (&bx)[S][2][NB])
 {
@@ -322,7 +322,16 @@ __device__ __forceinline__ void part_chunks(int C, int i, int n, int &c0, int &c
 // pass the XCD's own L2 by. A work group announces its stores by counters once they have completed:
 // then no cache has to be written back, which a release fence would do for the whole L2.
 __device__ __forceinline__ void store_shared(float *p, float v) { __hip_atomic_store(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
-__device__ __forceinline__ float load_shared(const float *p) { return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+__device__ __forceinline__ void store_shared(float *p, float v, float w)   // two in a row, 8-byte aligned
+{
+    const uint64_t u = (uint64_t)__float_as_uint(w) << 32 | __float_as_uint(v);
+    __hip_atomic_store(reinterpret_cast<uint64_t *>(p), u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ float2 load_shared2(const float *p)
+{
+    const uint64_t u = __hip_atomic_load(reinterpret_cast<const uint64_t *>(p), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    return make_float2(__uint_as_float((uint32_t)u), __uint_as_float((uint32_t)(u >> 32)));
+}
 
 // Work groups take contiguous shares [it0, it1) of (group, 16 rows) items; their sums add up to the
 // output. Each keeps its items' sums in LDS (`room` floats; what does not fit is passed on at once:
@@ -359,11 +368,17 @@ struct Partials {
     __device__ __forceinline__ void combine(int *todo, Out out) const
     {
         __syncthreads();
+        // two rows of a token to a thread (rows are a multiple of 8)
         const int per = T * kRows, all = min(it1 - it0, room / per) * per;
-        for (int i = threadIdx.x; i < all; i += kThreads) {
+        for (int i = threadIdx.x * 2; i < all; i += kThreads * 2) {
             const int it = it0 + i / per, t = i % per / kRows, r = i % kRows, row = it % rbs * kRows + r;
-            if (row < rows && groups == 1) out(t, row, kept[i]);
-            else if (row < rows) store_shared(partial + at(it, t, r), kept[i]);
+            if (row >= rows) continue;
+            if (groups > 1) {
+                store_shared(partial + at(it, t, r), kept[i], kept[i + 1]);
+            } else {
+                out(t, row, kept[i]);
+                out(t, row + 1, kept[i + 1]);
+            }
         }
         if (groups == 1) return;
         asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");   // all waves' stores have completed
@@ -377,14 +392,26 @@ struct Partials {
             todo[threadIdx.x] = rb;
             __syncthreads();
             const int n = min(it1 - base, kThreads) * per;
-            for (int i = threadIdx.x; i < n; i += kThreads) {
+            for (int i = threadIdx.x * 2; i < n; i += kThreads * 2) {
                 const int b = todo[i / per], t = i % per / kRows, row = b * kRows + i % kRows;
                 if (b < 0 || row >= rows) continue;
                 const float *p = partial + (size_t)t * rows + row;
-                float v = 0.f;
-#pragma unroll 8
-                for (int g = 0; g < groups; ++g) v += load_shared(p + (size_t)g * T * rows);
+                const size_t step = (size_t)T * rows;
+                // 16 groups' loads in flight (past the last: that one's again)
+                constexpr int kFlight = 16;
+                float v = 0.f, w = 0.f;
+                for (int g = 0; g < groups; g += kFlight) {
+                    float2 u[kFlight];
+#pragma unroll
+                    for (int j = 0; j < kFlight; ++j) u[j] = load_shared2(p + (size_t)min(g + j, groups - 1) * step);
+#pragma unroll
+                    for (int j = 0; j < kFlight; ++j) {
+                        v += g + j < groups ? u[j].x : 0.f;
+                        w += g + j < groups ? u[j].y : 0.f;
+                    }
+                }
                 out(t, row, v);
+                out(t, row + 1, w);
             }
             __syncthreads();
         }
