@@ -60,6 +60,7 @@ extern "C" {
 #define MOE_ADAPTER_MAX_TOKENS 65536  /* tokens per call of moe_adapter_project */
 #define MOE_ADAPTER_MAX_RANK 128
 #define MOE_ADAPTER_MAX_D (1 << 20)   /* moe_adapter_project: d_in and d_out upper bound */
+#define MOE_ADAPTER_MAX_STRIDE (1 << 26)   /* and of its row strides (elements) */
 
 /* Type of activations (x, y_in and y) of the functions that take one. */
 #define MOE_F32  0
@@ -291,9 +292,10 @@ typedef struct moe_adapter_desc {
  * block of tokens that uses it. A token whose adapters[t] is outside [0, n_adapters) has none.
  * Any order of tokens is right; those of one adapter side by side are fastest.
  * x, y_in, y   device, rows of d_in / d_out values of act_type (MOE_F32 or MOE_BF16), row strides
- *              in elements (multiples of 8); y_in may be NULL (zero) or y itself. fp32 activations
- *              enter the products exactly (three bf16 parts, so beyond 16 tokens an fp32 call does
- *              three times a bf16 call's matrix work); sums are fp32, a bf16 y is rounded once.
+ *              in elements (multiples of 8, at most MOE_ADAPTER_MAX_STRIDE); y_in may be NULL
+ *              (zero) or y itself, x must not overlap y. fp32 activations enter the products
+ *              exactly (three bf16 parts, so beyond 16 tokens an fp32 call does three times a
+ *              bf16 call's matrix work); sums are fp32, a bf16 y is rounded once.
  * adapters     device int32 [T]
  * workspace    device, 256-byte aligned, >= moe_adapter_workspace_bytes(T, d_in, d_out, rank,
  *              act_type); its content before the call does not matter. Calls that may run at the

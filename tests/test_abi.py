@@ -481,7 +481,8 @@ def _adapter_call(T=2, d=64, o=64, n=4, r=8, act=0, ws=256, nbytes=1 << 40, x=25
     (dict(r=12), b"rank=12"), (dict(r=136), b"rank=136"), (dict(x=None), b"null pointer"), (dict(y=None), b"null pointer"),
     (dict(ids=None), b"null pointer"), (dict(a=None), b"null pointer"), (dict(b=None), b"null pointer"),
     (dict(ws=None), b"null pointer"), (dict(xs=56), b"x_stride=56"), (dict(xs=68), b"x_stride=68"), (dict(ys=60), b"y_stride=60"),
-    (dict(y_in=512, yis=32), b"y_in_stride=32"), (dict(y_in=256, yis=72), b"another stride"), (dict(x=264), b"16-byte aligned"),
+    (dict(xs=(1 << 26) + 8), b"x_stride=67108872"), (dict(ys=(1 << 26) + 8), b"y_stride=67108872"),
+    (dict(y_in=512, yis=32), b"y_in_stride=32"), (dict(y_in=512, yis=(1 << 26) + 8), b"y_in_stride=67108872"), (dict(y_in=256, yis=72), b"another stride"), (dict(x=264), b"16-byte aligned"),
     (dict(y=264), b"16-byte aligned"), (dict(w=8), b"16-byte aligned"), (dict(a=8), b"16-byte aligned"),
     (dict(b=8), b"16-byte aligned"), (dict(ws=128), b"256-byte aligned"), (dict(nbytes=0), b"workspace 0 <"),
 ])
@@ -501,3 +502,18 @@ def test_adapter_workspace_sizes():
     for bad in ((0, 64, 64, 8, 0), (65537, 64, 64, 8, 0), (1, 0, 64, 8, 0), (1, 64, 64, 136, 0), (1, 64, 64, 8, 2)):
         assert moe.lib().moe_adapter_workspace_bytes(*bad) == 0
     assert moe.adapter_workspace_bytes(1, 64, 64, 8, torch.float16) == 0
+
+
+def test_device_calls_refuse_host_tensors():
+    import torch
+    x, ws = torch.zeros(2, 64), torch.zeros(1 << 20, dtype=torch.uint8)
+    with pytest.raises(ValueError, match="x must be on the GPU"):
+        moe.layer_tokens(x, torch.zeros(4, 64), ws, 64, 2, x.clone(), ws)
+    a = torch.zeros(3, 8, 64, dtype=torch.bfloat16)
+    with pytest.raises(ValueError, match="x must be on the GPU"):
+        moe.adapter_project(x, None, a, torch.zeros(3, 64, 8, dtype=torch.bfloat16), torch.zeros(2, dtype=torch.int32),
+                            x.clone(), ws)
+    with pytest.raises(ValueError, match="float32 or bfloat16"):
+        moe.layer_tokens(x.half(), torch.zeros(4, 64), ws, 64, 2, x.half(), ws)
+    with pytest.raises(ValueError, match="float32 or bfloat16"):
+        moe.adapter_project(x.half(), None, a, a, torch.zeros(2, dtype=torch.int32), x.half(), ws)

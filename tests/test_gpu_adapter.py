@@ -255,6 +255,30 @@ def test_offsets_beyond_32_bits():
         assert torch.equal(c2.run(), y)
 
 
+def test_arguments():
+    """Tensors the kernels could not read as they are refused by name; no tokens are no call."""
+    torch = torch_cuda()
+    say("adapter arguments")
+    c = Case(torch, 1, 5, 64, 128, 8, 3, "bfloat16")
+    y = torch.empty((5, 128), dtype=torch.bfloat16, device="cuda")
+    good = dict(x=c.x, w=c.w, a=c.a, b=c.b, adapters=c.ids, y=y, workspace=c.workspace(), scale=c.scale)
+    moe.adapter_project(**good)
+    wide = torch.zeros((5, 256), dtype=torch.bfloat16, device="cuda")
+    bad = [("x", dict(x=wide[:, :128:2])), ("y", dict(y=y.float())), ("y", dict(y=wide[:, ::2])), ("y_in", dict(y_in=y[:4])),
+           ("w", dict(w=c.w.float())), ("w", dict(w=c.w.t())), ("b", dict(b=c.b[:2])), ("a", dict(a=c.a.transpose(0, 1))),
+           ("adapters", dict(adapters=c.ids.long())), ("scale", dict(scale=c.scale[:2])),
+           ("workspace", dict(workspace=torch.empty(8, dtype=torch.uint8)))]
+    for name, change in bad:
+        with pytest.raises(ValueError, match=f"adapter_project: {name} must"):
+            moe.adapter_project(**{**good, **change})
+    with pytest.raises(moe.MoeError, match="x_stride=76"):
+        moe.adapter_project(**{**good, "x": torch.zeros((5, 76), dtype=torch.bfloat16, device="cuda")[:, :64]})
+    with pytest.raises(moe.MoeError, match="workspace"):
+        moe.adapter_project(**{**good, "workspace": good["workspace"][:256]})
+    none = torch.empty((0, 64), dtype=torch.bfloat16, device="cuda")
+    moe.adapter_project(none, c.w, c.a, c.b, c.ids[:0], y[:0], good["workspace"][:0])
+
+
 def test_a_batch_through_the_layer_and_its_adapted_shared_expert():
     """One decode step: the routed experts by layer_tokens, the shared expert's three projections
     by adapter_project straight out of its slab, each request with its adapters, the second on top

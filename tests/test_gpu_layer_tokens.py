@@ -296,3 +296,26 @@ def test_against_the_calls_it_replaces():
     assert np.array_equal(idx, ridx.cpu().numpy()) and np.allclose(w, rw.cpu().numpy(), rtol=2e-7, atol=0)
     err = (y - ref).abs().max() / ref.pow(2).mean().sqrt()
     assert float(err) <= 2.0 ** -16 * 4     # the other path keeps activations to 2^-18, twice
+
+
+def test_arguments():
+    """Tensors the kernels could not read as they are refused by name; no tokens are no call."""
+    torch = torch_cuda()
+    say("layer_tokens arguments")
+    layer = Layer(torch, 17, 64, 64, 4, 2, 64)
+    x = states(torch, 1, 3, 64, torch.float32)
+    y, ws = torch.empty_like(x), layer.workspace(3)
+    good = dict(x=x, w_router=layer.wr, slot_pool=layer.pool, f=64, k=2, y=y, workspace=ws, shared=layer.shared, f_shared=64)
+    moe.layer_tokens(**good)
+    bad = [("x", dict(x=torch.zeros((3, 128), device="cuda")[:, ::2])), ("y", dict(y=y.bfloat16())), ("y", dict(y=y[:2])),
+           ("y_in", dict(y_in=y.cpu())), ("w_router", dict(w_router=layer.wr.double())), ("slot_pool", dict(slot_pool=layer.pool[:3])),
+           ("slotmap", dict(slotmap=torch.zeros(3, dtype=torch.int32, device="cuda"))), ("shared", dict(shared=None)),
+           ("shared", dict(shared=layer.shared[:-128])), ("idx", dict(idx=torch.zeros((3, 2), device="cuda"))),
+           ("w", dict(w=torch.zeros((2, 3), device="cuda"))), ("workspace", dict(workspace=ws.cpu()))]
+    for name, change in bad:
+        with pytest.raises(ValueError, match=f"layer_tokens: {name} must"):
+            moe.layer_tokens(**{**good, **change})
+    with pytest.raises(moe.MoeError, match="workspace"):
+        moe.layer_tokens(**{**good, "workspace": ws[:256]})
+    none = torch.empty((0, 64), device="cuda")
+    moe.layer_tokens(none, layer.wr, layer.pool, 64, 2, none, ws[:0], shared=layer.shared, f_shared=64)
