@@ -519,7 +519,7 @@ __host__ __device__ inline int first_row(int T, int m, int mt)
 
 struct GemmParams {
     AdapterParams p;
-    int nk, steps;            // K steps of W; of a tile (times the activations' parts)
+    int steps;                // K steps of W
     uint16_t *vk;             // v in bf16, [T][vparts][rq * kBK]
     int vparts, rq;           // parts of v, K steps of its ranks
     int32_t *list;            // [mtiles][1 + kTileM] adapters of a tile: count, ids
@@ -555,16 +555,19 @@ __global__ __launch_bounds__(256) void k_adapter_parts(GemmParams g)
     for (int q = 0; q < g.vparts; ++q) g.vk[((size_t)t * g.vparts + q) * rp + j] = v_part(p.bf16, v, q);
 }
 
-// Rings of a tile of HB * 32 tokens: as many stages as LDS holds.
-template <int HB>
+// Blocks of 32 tokens of a tile, at most: a stage has room for 8 blocks of their parts.
+__host__ __device__ constexpr int tile_blocks(int parts) { return 8 / parts; }
+
+// Rings of a tile of EB * 32 token rows: as many stages as LDS holds.
+template <int EB>
 struct TileCfg {
-    static constexpr int kABytes = HB * 32 * kRowBytes;           // token rows of a stage
-    static constexpr int kAStages = HB <= 2 ? 4 : HB <= 5 ? 3 : 2;
-    static constexpr int kBStages = HB <= 2 ? 4 : 3;
+    static constexpr int kABytes = EB * 32 * kRowBytes;           // token rows of a stage
+    static constexpr int kAStages = EB <= 2 ? 4 : EB <= 5 ? 3 : 2;
+    static constexpr int kBStages = EB <= 2 ? 4 : 3;
     static constexpr int kBBase = kAStages * kABytes;
-    static constexpr int kALoads = (HB + 1) / 2;                  // load instructions per wave and stage
+    static constexpr int kALoads = (EB + 1) / 2;                  // load instructions per wave and stage
     static constexpr int kLoads = kALoads + kBLoads;
-    static constexpr int kRing = HB == 8 || HB == 6 || HB == 4 ? 4 : HB;   // divides 2 HB
+    static constexpr int kRing = EB == 8 || EB == 6 || EB == 4 ? 4 : EB;   // divides 2 EB
     static constexpr int kAhead = kRing < 4 ? kRing : 4;
     static constexpr int kKeep = kAStages == kBStages ? (kAStages - 2) * kLoads : kBLoads;
     static_assert(kBBase + kBStages * kBBytes <= kLdsBytes, "the rings fit LDS");
@@ -582,13 +585,17 @@ __device__ __forceinline__ void wait_and_barrier()
 // A tile of tokens row0 .. row0 + rows (up to HB * 32) by W rows nt * 256 ..: K steps k0 .. k0 +
 // nsteps, the adapters' steps too if `ext`. Two waves split the tokens and four the rows of W; both
 // operands go straight to LDS in rings of K steps, swizzled so that the operand reads touch all
-// banks evenly; one barrier per step (the same scheme as the experts' grouped products).
-template <bool kOnce, int HB>
+// banks evenly; one barrier per step (the same scheme as the experts' grouped products). Q: the
+// activations' parts; a step holds all of them, as Q * HB * 32 rows that share the sums, so that
+// a step of W is read once for them (with the parts as further K steps 333 tokens on 3592 x 2568 took
+// 81 us, 65 so).
+template <bool kOnce, int HB, int Q>
 __device__ __forceinline__ void project_tile(const GemmParams &g, uint8_t *lds, int row0, int rows, int nt, int mt, int k0,
                                              int nsteps, int start, bool ext, float *part)
 {
-    using C = TileCfg<HB>;
-    constexpr int NA = C::kAStages, NB = C::kBStages, P = C::kAhead, R = C::kRing, kItems = 2 * HB;
+    constexpr int EB = HB * Q;
+    using C = TileCfg<EB>;
+    constexpr int NA = C::kAStages, NB = C::kBStages, P = C::kAhead, R = C::kRing, kItems = 2 * EB;
     const AdapterParams &p = g.p;
     int lane = threadIdx.x & 63;
     asm volatile("" : "+v"(lane));   // keeps the addresses of all tile heights from being computed up front
@@ -597,14 +604,15 @@ __device__ __forceinline__ void project_tile(const GemmParams &g, uint8_t *lds, 
     const int lr = lane >> 3, lc = ((lane & 7) ^ lr) * 16;   // row of a load instruction, byte of its K step
     const int K2 = p.d * 2;
 
+    auto load_block = [&](int i) { return min(i * 8 + wv, EB * 4 - 1); };   // 8 rows of a load instruction
     auto token_row = [&](int i) {   // rows past the tile read its first
-        const int r = min(i * 8 + wv, HB * 4 - 1) * kLoadRows + lr;
+        const int r = load_block(i) % (HB * 4) * kLoadRows + lr;
         return row0 + (r < rows ? r : 0);
     };
     auto w_block = [&](int i) { return min(nt * kTileN + i * 64 + wv * kLoadRows, p.o - kLoadRows); };   // o % 8 == 0
     auto put_a = [&](int i, const uint8_t *src, int buf) {
         __builtin_amdgcn_global_load_lds((global_cvoid *)src,
-                                         (lds_void *)(lds + buf * C::kABytes + min(i * 8 + wv, HB * 4 - 1) * 1024), 16, 0, 0);
+                                         (lds_void *)(lds + buf * C::kABytes + load_block(i) * 1024), 16, 0, 0);
     };
     auto put_b = [&](int i, const uint8_t *src, int buf) {
         __builtin_amdgcn_global_load_lds((global_cvoid *)src, (lds_void *)(lds + C::kBBase + buf * kBBytes + (i * 8 + wv) * 1024),
@@ -612,7 +620,7 @@ __device__ __forceinline__ void project_tile(const GemmParams &g, uint8_t *lds, 
     };
     const uint8_t *asrc[C::kALoads];
 #pragma unroll
-    for (int j = 0; j < C::kALoads; ++j) asrc[j] = reinterpret_cast<const uint8_t *>(p.xk + token_row(j) * p.ldk) + lc;
+    for (int j = 0; j < C::kALoads; ++j) asrc[j] = reinterpret_cast<const uint8_t *>(p.xk + token_row(j) * p.ldk + load_block(j) / (HB * 4) * p.kpart) + lc;
     const uint32_t wlane = (uint32_t)lr * K2;
     auto step_of = [&](int stage) {   // steps go round from `start`
         const int ks = stage + start;
@@ -620,10 +628,8 @@ __device__ __forceinline__ void project_tile(const GemmParams &g, uint8_t *lds, 
     };
     auto load_a = [&](int i, int stage, int buf) { put_a(i, asrc[i] + (size_t)step_of(stage) * kRowBytes, buf); };
     auto load_b = [&](int i, int stage, int buf) {
-        int ks = step_of(stage);
-        while (ks >= g.nk) ks -= g.nk;   // the parts of the activations meet the same rows of W
         // past a row's end its last 16 bytes are read; the activations are zero there
-        put_b(i, p.w + (size_t)w_block(i) * K2 + (wlane + (uint32_t)min(ks * kRowBytes + lc, K2 - 16)), buf);
+        put_b(i, p.w + (size_t)w_block(i) * K2 + (wlane + (uint32_t)min(step_of(stage) * kRowBytes + lc, K2 - 16)), buf);
     };
 
     floatx4_t acc[HB][4];
@@ -633,24 +639,24 @@ __device__ __forceinline__ void project_tile(const GemmParams &g, uint8_t *lds, 
         for (int nb = 0; nb < 4; ++nb) acc[m][nb] = floatx4_t{0.f, 0.f, 0.f, 0.f};
 
     // Operand reads: row lane % 16 of a block, chunk 4 kb + lane / 16. The items of a step are
-    // (kb, m) in order; item j's token block is read P items before its MFMAs.
+    // (kb, part, m) in order; item j's token block is read P items before its MFMAs.
     const int rd = (lane & 15) * kRowBytes + ((lane >> 4) ^ (lane & 7)) * 16;
     const uint8_t *const ra = lds + wm * HB * 16 * kRowBytes;
     const uint8_t *const rb = lds + C::kBBase + wn * 64 * kRowBytes;
     bf16x8_t wf[2][4], tf[R];
     auto read_item = [&](int j, int ba, int bb) {
-        const int kb = j / HB, sl = rd ^ (kb * 64);
-        if (j % HB == 0) {
+        const int kb = j / EB, e = j % EB, sl = rd ^ (kb * 64);
+        if (e == 0) {
 #pragma unroll
             for (int nb = 0; nb < 4; ++nb)
                 wf[kb][nb] = *reinterpret_cast<const bf16x8_t *>(rb + bb * kBBytes + nb * 16 * kRowBytes + sl);
         }
-        tf[j % R] = *reinterpret_cast<const bf16x8_t *>(ra + ba * C::kABytes + (j % HB) * 16 * kRowBytes + sl);
+        tf[j % R] = *reinterpret_cast<const bf16x8_t *>(ra + ba * C::kABytes + (e / HB * HB * 32 + e % HB * 16) * kRowBytes + sl);
     };
     auto mma = [&](int j, const bf16x8_t t) {
 #pragma unroll
         for (int nb = 0; nb < 4; ++nb)
-            acc[j % HB][nb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wf[j / HB][nb], t, acc[j % HB][nb], 0, 0, 0);
+            acc[j % HB][nb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wf[j / EB][nb], t, acc[j % HB][nb], 0, 0, 0);   // (HB divides EB)
     };
     if (nsteps > 0) {
 #pragma unroll
@@ -791,7 +797,7 @@ __device__ __forceinline__ void project_tile(const GemmParams &g, uint8_t *lds, 
 
 // One work group per CU, looping over its tiles; the M tile fastest, eight contiguous runs of
 // tiles for the eight XCDs. kOnce: W is read once (one tile of tokens).
-template <bool kOnce>
+template <bool kOnce, int Q>
 __global__ __launch_bounds__(kThreads) void k_adapter_gemm(GemmParams g)
 {
     __shared__ __align__(1024) uint8_t lds[kLdsBytes];
@@ -816,7 +822,7 @@ __global__ __launch_bounds__(kThreads) void k_adapter_gemm(GemmParams g)
         const bool ext = ks == parts - 1;
         switch ((rows + 31) >> 5) {
 #define MOE_HB_CASE(N) \
-    case N: project_tile<kOnce, N>(g, lds, row0, rows, nt, mt, k0, kn, start, ext, part); break;
+    case N: if constexpr (N <= tile_blocks(Q)) project_tile<kOnce, N, Q>(g, lds, row0, rows, nt, mt, k0, kn, start, ext, part); break;
             MOE_HB_CASE(1) MOE_HB_CASE(2) MOE_HB_CASE(3) MOE_HB_CASE(4)
             MOE_HB_CASE(5) MOE_HB_CASE(6) MOE_HB_CASE(7) MOE_HB_CASE(8)
 #undef MOE_HB_CASE
@@ -1000,15 +1006,14 @@ struct Cut {
     int64_t cost;
 };
 // What a cut into m tiles of tokens costs, in ns, for the XCD with the most tiles: a K step of a tile
-// takes 250 ns and 6.65 a token (256 tokens: 1.95 us, 128: 1.1), a tile about 3 us beside its steps,
+// takes 250 ns and 6.65 a row of tokens' parts (256 rows: 1.95 us, 128: 1.1), a tile about 3 us beside its steps,
 // and a part's sums are written and read again, 40 ns a token, with another launch at the end.
-// (512 tokens on 4096 x 14336: 97 us with tiles of 128 tokens, 134 with 256; 333 fp32 tokens on 3592 x
-// 2568: 82 with four tiles, 100 with two.)
-Cut cost_of(int T, int m, int ntiles, int steps, int slots, size_t part_bytes)
+// (512 tokens on 4096 x 14336: 97 us with tiles of 128 tokens, 134 with 256.)
+Cut cost_of(int T, int m, int parts, int ntiles, int steps, int slots, size_t part_bytes)
 {
     const int rows = std::min(T, ceil_div(ceil_div(T, 32), m) * 32);
     const int units = ceil_div((int64_t)m * ntiles, kXcds), full = units / slots, left = units % slots;
-    const int64_t step = 250 + 665 * rows / 100, tile = 3000;
+    const int64_t step = 250 + 665 * rows * parts / 100, tile = 3000;
     const int maxparts = (int)std::min<size_t>(kMaxParts, part_bytes / ((size_t)kXcds * rows * kTileN * 4));
     Cut c{m, 1, (int64_t)(full + (left > 0)) * (steps * step + tile)};
     for (int s = 2; s <= kMaxSplit && left > 0 && s * kMinPartSteps <= steps && left * s <= maxparts; ++s) {
@@ -1020,13 +1025,13 @@ Cut cost_of(int T, int m, int ntiles, int steps, int slots, size_t part_bytes)
     }
     return c;
 }
-// The cheapest: tiles of 256 tokens down to 32.
-Cut best_cut(int T, int ntiles, int steps, int slots, size_t part_bytes)
+// The cheapest, from the tallest tiles down to 32 tokens.
+Cut best_cut(int T, int parts, int ntiles, int steps, int slots, size_t part_bytes)
 {
-    Cut best = cost_of(T, tiles_of(T), ntiles, steps, slots, part_bytes);
-    for (int h = 7; h >= 1; --h) {
-        const Cut c = cost_of(T, std::max(1, ceil_div(T, 32 * h)), ntiles, steps, slots, part_bytes);
-        if (c.cost < best.cost) best = c;
+    Cut best{};
+    for (int h = tile_blocks(parts); h >= 1; --h) {
+        const Cut c = cost_of(T, ceil_div(T, 32 * h), parts, ntiles, steps, slots, part_bytes);
+        if (best.mtiles == 0 || c.cost < best.cost) best = c;
     }
     return best;
 }
@@ -1050,15 +1055,14 @@ hipError_t launch_gemm(AdapterParams p, const AdapterPlan &L, uint8_t *ws, hipSt
     if (p.n > 0 && (e = launch_shrink(p, L, s)) != hipSuccess) return e;
     GemmParams g{};
     g.p = p;
-    g.nk = L.nk;
-    g.steps = p.w ? parts * L.nk : 0;
+    g.steps = p.w ? L.nk : 0;
     g.vk = reinterpret_cast<uint16_t *>(ws + L.vk);
     g.vparts = L.vparts;
     g.rq = L.rq;
     g.list = reinterpret_cast<int32_t *>(ws + L.list);
     g.ntiles = ceil_div(p.o, kTileN);
     g.slots = std::max(1, device_cu_count() / kXcds);
-    const Cut cut = best_cut(p.T, g.ntiles, g.steps, g.slots, L.part_bytes);
+    const Cut cut = best_cut(p.T, parts, g.ntiles, g.steps, g.slots, L.part_bytes);
     g.mtiles = cut.mtiles;
     g.prows = std::min(p.T, ceil_div(ceil_div(p.T, 32), g.mtiles) * 32);
     g.maxparts = (int)std::min<size_t>(kMaxParts, L.part_bytes / ((size_t)kXcds * g.prows * kTileN * 4));
@@ -1074,8 +1078,10 @@ hipError_t launch_gemm(AdapterParams p, const AdapterPlan &L, uint8_t *ws, hipSt
         tail = tail || (g.plan[x].s > 1 && g.plan[x].units > g.plan[x].full);
     }
     const dim3 grid(kXcds * g.slots);
-    if (g.mtiles == 1) hipLaunchKernelGGL(k_adapter_gemm<true>, grid, dim3(kThreads), 0, s, g);
-    else hipLaunchKernelGGL(k_adapter_gemm<false>, grid, dim3(kThreads), 0, s, g);
+    if (p.bf16 && g.mtiles == 1) hipLaunchKernelGGL((k_adapter_gemm<true, 1>), grid, dim3(kThreads), 0, s, g);
+    else if (p.bf16) hipLaunchKernelGGL((k_adapter_gemm<false, 1>), grid, dim3(kThreads), 0, s, g);
+    else if (g.mtiles == 1) hipLaunchKernelGGL((k_adapter_gemm<true, 3>), grid, dim3(kThreads), 0, s, g);
+    else hipLaunchKernelGGL((k_adapter_gemm<false, 3>), grid, dim3(kThreads), 0, s, g);
     if ((e = hipGetLastError()) != hipSuccess || !tail) return e;
     hipLaunchKernelGGL(k_adapter_tail, dim3((unsigned)(kXcds * g.slots * ceil_div(g.prows, kTailRows))), dim3(256), 0, s, g);
     return hipGetLastError();
