@@ -12,8 +12,8 @@
 //   longer:
 //   1. cast: the activations as bf16 parts, where they are fp32 or their rows do not end with a K
 //      step;
-//   2. shrink: v, per block of tokens: the adapters among them, each a few blocks of 16 rows of
-//      A, are multiplied with all the block's tokens; a token keeps its own adapter's sums;
+//   2. shrink: v, per block of tokens: for each adapter among them, 16 to 64 rows of its A are held
+//      and the block's tokens, 16 at a time where one holds the adapter, streamed past them;
 //   3. parts: v scaled and cut into bf16 parts, and the adapters in every tile of tokens;
 //   4. gemm: tiles of up to 256 tokens by 256 rows of W; after the K steps of W, each adapter
 //      in the tile adds a few more: its B rows against the tile's v, the products kept by its own
@@ -384,19 +384,23 @@ struct BlockIds {
 };
 
 // The items of a work group: its adapters of the block (every step-th of the list), for each the
-// ranks 64 at a time, the block's 16 tokens at a time that hold it, and the activations' parts.
+// ranks 16 NB at a time: NB times 16 rows of A, then the block's 16 tokens at a time that hold the
+// adapter, and of those the activations' parts.
+template <int NB>
 struct ShrinkSrc {
+    static constexpr int kRanks = NB * 16;
     const AdapterParams &p;
     const BlockIds &ids;
     const int32_t *list;
     int t0, j, step, nlist, halves, parts, cnt;
-    int half, q;              // of the next item
+    int half, nb, q;          // of the next item
     uint32_t left;            // its adapter's 16 tokens still to come, this one the lowest
+    int token_lane, a_lane;   // byte offset of this lane's row among 8 of the tokens', of A's
     Rows r;
-    // Moves to the first item of adapter j on that has any.
+    // Moves to the first item of adapter j.
     __device__ __forceinline__ void adapter()
     {
-        half = q = 0;
+        half = nb = q = 0;
         left = j < nlist ? ids.sixteens(list[j]) : 0;
     }
     __device__ __forceinline__ int first_token() const { return min(t0 + __builtin_ctz(left) * 16, p.T - 16); }   // (T > 16)
@@ -404,16 +408,30 @@ struct ShrinkSrc {
     {
         r.cnt = j < nlist ? cnt : 0;
         if (j >= nlist) return r;
+        if (nb < NB) {
+            const int row = min(half * kRanks + nb * 16, (p.r - 1) / 16 * 16);   // (blocks past the ranks are not used)
+            r.bytes = p.d * 2;
+            r.lane_row = a_lane;
+            r.base = p.a + ((size_t)list[j] * p.r + row) * r.bytes;
+            r.half = row + 8 < p.r ? (size_t)8 * r.bytes : 0;   // the last block may have 8 rows
+            ++nb;
+            return r;
+        }
+        r.bytes = chunks_of(p.d) * kChunk * 2;   // (a row of xk ends with a chunk)
+        r.lane_row = token_lane;
         r.base = reinterpret_cast<const uint8_t *>(p.xk + (size_t)first_token() * p.ldk + (size_t)q * p.kpart);
+        r.half = (size_t)p.ldk * 16;
         step_on();
         return r;
     }
+    // Past the current part of 16 tokens.
     __device__ __forceinline__ void step_on()
     {
         if (++q < parts) return;
         q = 0;
         left &= left - 1;
         if (left) return;
+        nb = 0;
         if (++half < halves) {
             left = ids.sixteens(list[j]);
             return;
@@ -425,13 +443,15 @@ struct ShrinkSrc {
 
 // v of the tokens of block x, K group y, of the block's adapters every gridDim.z-th. Here the tokens'
 // rows are streamed, 16 at a time, as the A operand, and 16 NB rows of an adapter's A stay in
-// registers as the columns, so that a token's row is read once for each adapter near it. (With the
-// tokens in registers and the A rows streamed past every 64 of them, 4096 tokens of 14336 values and
-// rank 64 took 77 us, 67 so.)
+// registers as the columns, so that a token's row is read once for each adapter near it: 4096 tokens
+// of 14336 values and rank 64 take 64 us. (With the tokens in registers and the A rows streamed past
+// every 64 of them 77; with A's rows loaded straight into the registers, 16 rows by 64 bytes per
+// instruction, instead of through the ring, 67.)
 template <int S, int NB>
 __global__ __launch_bounds__(kThreads) void k_adapter_shrink(AdapterParams p)
 {
-    using Stream_t = Stream<S, ShrinkSrc>;
+    using Src = ShrinkSrc<NB>;
+    using Stream_t = Stream<S, Src>;
     __shared__ __align__(1024) uint8_t lds[kWaves * Stream_t::kBytes];
     __shared__ __align__(16) Sums<NB> sums;
     __shared__ int32_t list[kBlockTokens];
@@ -451,43 +471,33 @@ __global__ __launch_bounds__(kThreads) void k_adapter_shrink(AdapterParams p)
     __syncthreads();
     const int adapters = __builtin_amdgcn_readfirstlane(nlist);
     if ((int)blockIdx.z >= adapters) return;
-    constexpr int kRanks = NB * 16;
     const int chunks = chunks_of(p.d), units = (chunks + S - 1) / S;
     int c0, cnt;
     unit_chunks(chunks, g * kWaves + wv, units, c0, cnt);
-    ShrinkSrc src{p, ids, list, t0, (int)blockIdx.z, (int)gridDim.z, adapters, (p.r + kRanks - 1) / kRanks, x_parts(p.bf16), cnt, 0, 0, 0, {}};
-    src.r.bytes = chunks * kChunk * 2;   // (a row of xk ends with a chunk)
-    src.r.lane_row = lane_row_of((int)(p.ldk * 2));
-    src.r.half = (size_t)p.ldk * 16;
+    Src src{p, ids, list, t0, (int)blockIdx.z, (int)gridDim.z, adapters, (p.r + Src::kRanks - 1) / Src::kRanks, x_parts(p.bf16), cnt,
+            0, 0, 0, 0, lane_row_of((int)(p.ldk * 2)), lane_row_of(p.d * 2), {}};
     src.r.c0 = c0;
     src.adapter();
-    ShrinkSrc at = src;                  // of the item that is multiplied
+    Src at = src;                        // of the item that is multiplied
     Stream_t st;
     st.start(src, lds + wv * Stream_t::kBytes, reinterpret_cast<const uint8_t *>(p.xk));
     bf16x8_t bx[S][2][NB];
     for (int j = -1, half = -1, n = 0; at.j < adapters;) {
         const int a = list[at.j], h = at.half, t = at.first_token();
-        if (at.j != j || h != half) {    // this adapter's rows of A
+        if (at.j != j || h != half) {    // this adapter's rows of A: as operands they are held alike
             j = at.j;
             half = h;
 #pragma unroll
             for (int nb = 0; nb < NB; ++nb) {
-                const int i = h * kRanks + nb * 16 + (lane & 15);
-                const uint16_t *row = reinterpret_cast<const uint16_t *>(p.a) + ((size_t)a * p.r + min(i, p.r - 1)) * p.d;
 #pragma unroll
-                for (int s = 0; s < S; ++s)
-#pragma unroll
-                    for (int kb = 0; kb < 2; ++kb)
-                        bx[s][kb][nb] = *reinterpret_cast<const bf16x8_t *>(row + min((c0 + s) * kChunk + kb * 32 + (lane >> 4) * 8, p.d - 8));
+                for (int s = 0; s < S; ++s) {
+                    bf16x8_t w[2];
+                    st.take(s, w);
+                    bx[s][0][nb] = s < cnt ? w[0] : no_tokens();
+                    bx[s][1][nb] = s < cnt ? w[1] : no_tokens();
+                }
+                st.advance(src);
             }
-#pragma unroll
-            for (int nb = 0; nb < NB; ++nb)
-#pragma unroll
-                for (int s = 0; s < S; ++s)
-#pragma unroll
-                    for (int kb = 0; kb < 2; ++kb)
-                        bx[s][kb][nb] = (c0 + s) * kChunk + kb * 32 + (lane >> 4) * 8 < p.d ? bx[s][kb][nb] : no_tokens();
-            settle(bx);
         }
         floatx4_t acc[NB];
         clear(acc);
@@ -500,8 +510,8 @@ __global__ __launch_bounds__(kThreads) void k_adapter_shrink(AdapterParams p)
         const int row = (wv & 3) * 4 + (lane >> 4);
 #pragma unroll
         for (int nb = 0; nb < (NB + 1) / 2; ++nb) {
-            const int c = (nb * 2 + (wv >> 2)) * 16 + (lane & 15), i = h * kRanks + c;
-            if (c < kRanks && i < p.r && mine[16 + t + row - t0] == a)
+            const int c = (nb * 2 + (wv >> 2)) * 16 + (lane & 15), i = h * Src::kRanks + c;
+            if (c < Src::kRanks && i < p.r && mine[16 + t + row - t0] == a)
                 p.v[((size_t)g * p.T + t + row) * p.r + i] = sums.template token<false>(n, row, c, 1, 1);
         }
         ++n;
