@@ -14,10 +14,11 @@
 //      step;
 //   2. shrink: v, per block of tokens: for each adapter among them, 16 to 64 rows of its A are held
 //      and the block's tokens, 16 at a time where one holds the adapter, streamed past them;
-//   3. parts: v scaled and cut into bf16 parts, and the adapters in every tile of tokens;
-//   4. gemm: tiles of up to 256 tokens by 256 rows of W; after the K steps of W, each adapter
-//      in the tile adds a few more: its B rows against the tile's v, the products kept by its own
-//      tokens. The tiles of a last, partial round of work groups are split over K, and
+//   3. join: v's K groups added up, where there are several;
+//   4. gemm: tiles of up to 256 tokens by 256 rows of W; after the K steps of W, the tile's v,
+//      scaled and in bf16 parts, stays in LDS and meets the B rows of each adapter in the tile, the
+//      products kept by its own tokens. The tiles of a last, partial round of work groups are split
+//      over K, and
 //   5. tail adds their parts.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
@@ -57,7 +58,7 @@ struct AdapterParams {
     int groups;
     // longer
     int tb, vgroups;              // tokens of a shrink block; K groups of v
-    float *v;                     // [vgroups][T][r], unscaled
+    float *v;                     // [vgroups][T][r], unscaled; the gemm takes the first group
     const uint16_t *xk;           // activations in bf16, their parts side by side: [T][ldk], a part kpart values
     int64_t ldk, kpart;
 };
@@ -330,30 +331,40 @@ __global__ __launch_bounds__(256) void k_adapter_cast(AdapterParams p, uint16_t 
     *reinterpret_cast<uint4 *>(xk + (size_t)t * p.ldk + (size_t)q * p.kpart + k) = v;
 }
 
-// The distinct adapters among `n` tokens (up to 64 K), in order of first appearance, by one wave.
+// The adapters of n tokens (up to 64 K) from t0 on, in every wave alike: lane l has tokens l, l + 64,
+// .. ; -1: none.
 template <int K>
-__device__ __forceinline__ int distinct(const AdapterParams &p, int t0, int n, int32_t *list)
+__device__ __forceinline__ void load_ids(const AdapterParams &p, int t0, int n, int (&id)[K])
 {
-    const int lane = threadIdx.x & 63;
-    int id[K], count = 0;
 #pragma unroll
     for (int k = 0; k < K; ++k) {
-        const int i = k * kWave + lane;
+        const int i = k * kWave + (threadIdx.x & 63);
         id[k] = i < n ? p.ids[t0 + i] : -1;
         if (!has_adapter(p, id[k])) id[k] = -1;
     }
+}
+// The first adapter of those, which is taken out; -1: there is none.
+template <int K>
+__device__ __forceinline__ int take_adapter(int (&id)[K])
+{
+    int a = -1;
 #pragma unroll
     for (int k = 0; k < K; ++k) {
-        uint64_t m = __ballot(id[k] >= 0);
-        while (m) {
-            const int a = __builtin_amdgcn_readlane(id[k], __builtin_ctzll(m));
-            if (lane == 0) list[count] = a;
-            ++count;
-#pragma unroll
-            for (int j = k; j < K; ++j) id[j] = id[j] == a ? -1 : id[j];
-            m = __ballot(id[k] >= 0);
-        }
+        const uint64_t m = __ballot(id[k] >= 0);
+        if (a < 0 && m) a = __builtin_amdgcn_readlane(id[k], __builtin_ctzll(m));
     }
+#pragma unroll
+    for (int k = 0; k < K; ++k) id[k] = id[k] == a ? -1 : id[k];
+    return a;
+}
+// The distinct ones into `list`, by one wave.
+template <int K>
+__device__ __forceinline__ int distinct(const AdapterParams &p, int t0, int n, int32_t *list)
+{
+    int id[K], count = 0;
+    load_ids(p, t0, n, id);
+    for (int a; (a = take_adapter(id)) >= 0; ++count)
+        if ((threadIdx.x & 63) == 0) list[count] = a;
     return count;
 }
 
@@ -361,14 +372,6 @@ __device__ __forceinline__ int distinct(const AdapterParams &p, int t0, int n, i
 struct BlockIds {
     static constexpr int K = kBlockTokens / kWave;
     int id[K];
-    __device__ __forceinline__ void load(const AdapterParams &p, int t0, int n)
-    {
-#pragma unroll
-        for (int k = 0; k < K; ++k) {
-            const int i = k * kWave + (threadIdx.x & 63);
-            id[k] = i < n ? p.ids[t0 + i] : -1;
-        }
-    }
     // Bit b: 16 tokens b of the block hold one of adapter a.
     __device__ __forceinline__ uint32_t sixteens(int a) const
     {
@@ -467,7 +470,7 @@ __global__ __launch_bounds__(kThreads) void k_adapter_shrink(AdapterParams p)
         mine[i] = t >= 0 && t < p.T ? p.ids[t] : -1;
     }
     BlockIds ids;
-    ids.load(p, t0, tn);
+    load_ids(p, t0, tn, ids.id);
     __syncthreads();
     const int adapters = __builtin_amdgcn_readfirstlane(nlist);
     if ((int)blockIdx.z >= adapters) return;
@@ -530,39 +533,40 @@ __host__ __device__ inline int first_row(int T, int m, int mt)
 struct GemmParams {
     AdapterParams p;
     int steps;                // K steps of W
-    uint16_t *vk;             // v in bf16, [T][vparts][rq * kBK]
-    int vparts, rq;           // parts of v, K steps of its ranks
-    int32_t *list;            // [mtiles][1 + kTileM] adapters of a tile: count, ids
     int mtiles, ntiles, slots;
     TilePlan plan[kXcds];
     int maxparts, prows;      // part buffers per XCD and their rows
     float *part;              // [8][maxparts][prows][kTileN]
 };
 
-// The tiles' lists, a wave each; then vk, 256 values of v per work group.
-__global__ __launch_bounds__(256) void k_adapter_parts(GemmParams g)
+// v of token t, 8 ranks from j on, scaled; zeros past the ranks and without an adapter.
+__device__ __forceinline__ void load_v(const AdapterParams &p, int t, int j, float (&v)[8])
 {
-    const AdapterParams &p = g.p;
-    const int lists = (g.mtiles + 3) / 4, wv = threadIdx.x >> 6;
-    if ((int)blockIdx.x < lists) {
-        const int b = blockIdx.x * 4 + wv;
-        if (b >= g.mtiles) return;
-        const int r0 = first_row(p.T, g.mtiles, b);
-        int32_t *list = g.list + (size_t)b * (kTileM + 1);
-        const int n = distinct<kTileM / kWave>(p, r0, first_row(p.T, g.mtiles, b + 1) - r0, list + 1);
-        if ((threadIdx.x & 63) == 0) list[0] = n;
-        return;
-    }
-    const int rp = g.rq * kBK;
-    const int64_t i = (int64_t)(blockIdx.x - lists) * 256 + threadIdx.x;
-    if (i >= (int64_t)p.T * rp) return;
-    const int t = (int)(i / rp), j = (int)(i - (int64_t)t * rp), id = p.ids[t];
-    float v = 0.f;
+    floatx4_t lo = floatx4_t{0.f, 0.f, 0.f, 0.f}, hi = lo;
+    const int id = p.ids[t];
     if (has_adapter(p, id) && j < p.r) {
-        for (int k = 0; k < p.vgroups; ++k) v += p.v[((size_t)k * p.T + t) * p.r + j];
-        v *= scale_of(p, id);
+        const floatx4_t *at = reinterpret_cast<const floatx4_t *>(p.v + (size_t)t * p.r + j);
+        lo = at[0] * scale_of(p, id);
+        hi = at[1] * scale_of(p, id);
     }
-    for (int q = 0; q < g.vparts; ++q) g.vk[((size_t)t * g.vparts + q) * rp + j] = v_part(p.bf16, v, q);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        v[i] = lo[i];
+        v[i + 4] = hi[i];
+    }
+}
+
+// v's K groups added up, into the first. (Where the tiles add them up themselves, 512 tokens on 4096 x
+// 14336 take as long, 4096 with rank 128 569 us instead of 546, 64 with 64 adapters of rank 128 177
+// instead of 173.)
+__global__ __launch_bounds__(256) void k_adapter_join(AdapterParams p)
+{
+    const size_t i = ((size_t)blockIdx.x * 256 + threadIdx.x) * 4, all = (size_t)p.T * p.r;   // (r is a multiple of 8)
+    if (i >= all) return;
+    floatx4_t s = *reinterpret_cast<const floatx4_t *>(p.v + i);
+#pragma unroll 4
+    for (int k = 1; k < p.vgroups; ++k) s += *reinterpret_cast<const floatx4_t *>(p.v + k * all + i);
+    *reinterpret_cast<floatx4_t *>(p.v + i) = s;
 }
 
 // Blocks of 32 tokens of a tile, at most: a stage has room for 8 blocks of their parts.
@@ -624,9 +628,8 @@ __device__ __forceinline__ void project_tile(const GemmParams &g, uint8_t *lds, 
         __builtin_amdgcn_global_load_lds((global_cvoid *)src,
                                          (lds_void *)(lds + buf * C::kABytes + load_block(i) * 1024), 16, 0, 0);
     };
-    auto put_b = [&](int i, const uint8_t *src, int buf) {
-        __builtin_amdgcn_global_load_lds((global_cvoid *)src, (lds_void *)(lds + C::kBBase + buf * kBBytes + (i * 8 + wv) * 1024),
-                                         16, 0, kOnce ? 2 : 0);   // 2: nontemporal
+    auto put_b = [&](int i, const uint8_t *src, uint8_t *to) {
+        __builtin_amdgcn_global_load_lds((global_cvoid *)src, (lds_void *)(to + (i * 8 + wv) * 1024), 16, 0, kOnce ? 2 : 0);   // 2: nontemporal
     };
     const uint8_t *asrc[C::kALoads];
 #pragma unroll
@@ -639,7 +642,8 @@ __device__ __forceinline__ void project_tile(const GemmParams &g, uint8_t *lds, 
     auto load_a = [&](int i, int stage, int buf) { put_a(i, asrc[i] + (size_t)step_of(stage) * kRowBytes, buf); };
     auto load_b = [&](int i, int stage, int buf) {
         // past a row's end its last 16 bytes are read; the activations are zero there
-        put_b(i, p.w + (size_t)w_block(i) * K2 + (wlane + (uint32_t)min(step_of(stage) * kRowBytes + lc, K2 - 16)), buf);
+        put_b(i, p.w + (size_t)w_block(i) * K2 + (wlane + (uint32_t)min(step_of(stage) * kRowBytes + lc, K2 - 16)),
+              lds + C::kBBase + buf * kBBytes);
     };
 
     floatx4_t acc[HB][4];
@@ -721,55 +725,88 @@ __device__ __forceinline__ void project_tile(const GemmParams &g, uint8_t *lds, 
     }
 
     if (ext) {
-        // The adapters' steps, two at a time. Every token's v meets every adapter of the tile; a
-        // step's products are added to the tokens of its adapter only (not by zeros in v: one
-        // request's infinite or NaN weights must not reach another's tokens).
-        const int32_t *list = g.list + (size_t)mt * (kTileM + 1);
-        const int per = g.vparts * g.rq, r2 = p.r * 2;
-        const int total = __builtin_amdgcn_readfirstlane(list[0]) * per;
-        int own[HB];
+        // The adapters: 64 ranks of the tile's v are put into LDS in bf16 parts, as token rows of a K
+        // step, and the B rows of as many adapters as fit beside them. Every token's v meets every
+        // adapter of the tile; the products are added to the tokens of that adapter only (not by
+        // zeros in v: one request's infinite or NaN weights must not reach another's tokens). (With
+        // v's parts made by a kernel of their own and loaded again for each adapter, 512 tokens of 9
+        // runs on 4096 x 14336 took 90 us, 86 so; 333 in fp32 on 3592 x 2568 64 and 57.)
+        constexpr int VP = Q == 1 ? 2 : 3, kVBytes = HB * 32 * kRowBytes, kFit = (kLdsBytes - VP * kVBytes) / kBBytes;
+        constexpr int kRound = kFit < 4 ? kFit : 4, kIds = (HB * 32 + kWave - 1) / kWave;
+        uint8_t *const bst = lds + VP * kVBytes;
+        int id[kIds], own[HB];
+        load_ids(p, row0, rows, id);
 #pragma unroll
         for (int m = 0; m < HB; ++m) own[m] = p.ids[row0 + min((wm * HB + m) * 16 + (lane & 15), rows - 1)];
-        for (int e = 0; e < total; e += 2) {
-            wait_and_barrier<0>();   // what LDS holds is read
+        const int r2 = p.r * 2;
+        int left[kIds], a[kRound];
+        auto adapter = [&](int u) { return u == 0 ? a[0] : u == 1 ? a[1] : u == 2 ? a[2] : a[kRound - 1]; };
+        auto next_round = [&](int rc) {   // false: there is none
 #pragma unroll
-            for (int u = 0; u < 2; ++u) {
-                if (e + u >= total) break;
-                const int a = __builtin_amdgcn_readfirstlane(list[1 + (e + u) / per]), q = (e + u) % per, rc = q % g.rq;
+            for (int u = 0; u < kRound; ++u) a[u] = take_adapter(left);
+            if (a[0] < 0) return false;
+            wait_and_barrier<0>();        // what LDS holds is read
+#pragma unroll 1
+            for (int u = 0; u < kRound && adapter(u) >= 0; ++u) {
 #pragma unroll
-                for (int i = 0; i < C::kALoads; ++i)
-                    put_a(i, reinterpret_cast<const uint8_t *>(g.vk + ((size_t)token_row(i) * per + q) * kBK) + lc, u);
-#pragma unroll
-                for (int i = 0; i < kBLoads; ++i)
-                    put_b(i, p.b + ((size_t)a * p.o + w_block(i)) * r2 + (uint32_t)(lr * r2 + min(rc * kRowBytes + lc, r2 - 16)), u);
+                for (int i = 0; i < kBLoads; ++i)   // (past the ranks v is zero)
+                    put_b(i, p.b + ((size_t)adapter(u) * p.o + w_block(i)) * r2 + (uint32_t)(lr * r2 + min(rc * kRowBytes + lc, r2 - 16)),
+                          bst + u * kBBytes);
             }
-            wait_and_barrier<0>();
+            return true;
+        };
+#pragma unroll 1
+        for (int rc = 0; rc * kBK < p.r; ++rc) {
 #pragma unroll
-            for (int u = 0; u < 2; ++u) {
-                if (e + u >= total) break;
-                const int a = __builtin_amdgcn_readfirstlane(list[1 + (e + u) / per]);
-                bf16x8_t w[2][4];
+            for (int k = 0; k < kIds; ++k) left[k] = id[k];
+            if (!next_round(rc)) break;
+#pragma unroll 1
+            for (int i = threadIdx.x; i < HB * 32 * (kBK / 8); i += kThreads) {
+                const int tr = i / (kBK / 8), c = i % (kBK / 8);
+                float v[8];
+                load_v(p, row0 + min(tr, rows - 1), rc * kBK + c * 8, v);
 #pragma unroll
-                for (int kb = 0; kb < 2; ++kb)
+                for (int q = 0; q < VP; ++q) {
+                    uint32_t w[4];
 #pragma unroll
-                    for (int nb = 0; nb < 4; ++nb)
-                        w[kb][nb] = *reinterpret_cast<const bf16x8_t *>(rb + u * kBBytes + nb * 16 * kRowBytes + (rd ^ (kb * 64)));
-#pragma unroll
-                for (int m = 0; m < HB; ++m) {
-                    bf16x8_t v[2];
-#pragma unroll
-                    for (int kb = 0; kb < 2; ++kb)
-                        v[kb] = *reinterpret_cast<const bf16x8_t *>(ra + u * C::kABytes + m * 16 * kRowBytes + (rd ^ (kb * 64)));
-#pragma unroll
-                    for (int nb = 0; nb < 4; ++nb) {
-                        floatx4_t d = floatx4_t{0.f, 0.f, 0.f, 0.f};
-                        d = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w[0][nb], v[0], d, 0, 0, 0);
-                        d = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w[1][nb], v[1], d, 0, 0, 0);
-#pragma unroll
-                        for (int c = 0; c < 4; ++c) acc[m][nb][c] += own[m] == a ? d[c] : 0.f;
-                    }
+                    for (int j = 0; j < 4; ++j) w[j] = part_of<VP>(v[2 * j], q) | (uint32_t)part_of<VP>(v[2 * j + 1], q) << 16;
+                    *reinterpret_cast<uint4 *>(lds + q * kVBytes + tr * kRowBytes + (c ^ (tr & 7)) * 16) = make_uint4(w[0], w[1], w[2], w[3]);
                 }
             }
+#pragma unroll 1
+            do {
+                wait_and_barrier<0>();
+#pragma unroll 1
+                for (int u = 0; u < kRound && adapter(u) >= 0; ++u) {
+                    const int now = adapter(u);
+                    asm volatile("" ::: "memory");   // v is read anew: held for the next adapter it would not fit the registers
+                    bf16x8_t w[2][4];
+#pragma unroll
+                    for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+                        for (int nb = 0; nb < 4; ++nb)
+                            w[kb][nb] = *reinterpret_cast<const bf16x8_t *>(bst + u * kBBytes + (wn * 64 + nb * 16) * kRowBytes + (rd ^ (kb * 64)));
+#pragma unroll
+                    for (int m = 0; m < HB; ++m) {
+                        floatx4_t d[4];
+#pragma unroll
+                        for (int nb = 0; nb < 4; ++nb) d[nb] = floatx4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                        for (int q = 0; q < VP; ++q)
+#pragma unroll
+                            for (int kb = 0; kb < 2; ++kb) {
+                                const bf16x8_t v = *reinterpret_cast<const bf16x8_t *>(ra + q * kVBytes + m * 16 * kRowBytes + (rd ^ (kb * 64)));
+#pragma unroll
+                                for (int nb = 0; nb < 4; ++nb) d[nb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w[kb][nb], v, d[nb], 0, 0, 0);
+                            }
+#pragma unroll
+                        for (int nb = 0; nb < 4; ++nb)
+#pragma unroll
+                            for (int c = 0; c < 4; ++c) acc[m][nb][c] += own[m] == now ? d[nb][c] : 0.f;
+                        __builtin_amdgcn_sched_barrier(0);   // (not all the reads first)
+                    }
+                }
+            } while (next_round(rc));
         }
     }
 
@@ -918,10 +955,10 @@ StreamPlan shrink_plan(int T, int d, int r, int *tb)
 struct AdapterPlan {
     StreamPlan stream;         // of the rows (up to 16 tokens) or of shrink
     bool gemm, copy;
-    int tb, nk, vparts, rq;
+    int tb, nk;
     size_t part_bytes;
     size_t xc, vc, partial, counts;            // up to 16 tokens
-    size_t xk, v, vk, list, part, bytes;       // longer
+    size_t xk, v, part, bytes;                 // longer
 };
 
 AdapterPlan plan_adapter(int T, int d, int o, int r, bool bf16)
@@ -934,24 +971,20 @@ AdapterPlan plan_adapter(int T, int d, int o, int r, bool bf16)
         at += a256(b);
         return was;
     };
-    L.vparts = v_parts(bf16);
     L.gemm = T > kStreamTokens;
     if (!L.gemm) {
         L.stream = stream_plan(d, column_blocks(parts, T));
         L.xc = take((size_t)chunks_of(d) * kChunk * T * parts * 2);
-        L.vc = take((size_t)L.vparts * T * chunks_of(r) * kChunk * 2);
+        L.vc = take((size_t)v_parts(bf16) * T * chunks_of(r) * kChunk * 2);
         L.partial = take(L.stream.groups > 1 ? (size_t)L.stream.groups * T * o * 4 : 0);
         L.counts = take((size_t)ceil_div(o, kRows) * 4);
     } else {
         L.stream = shrink_plan(T, d, r, &L.tb);
         L.nk = ceil_div(d, kBK);
         L.copy = !bf16 || d % kBK != 0;   // bf16 rows that end with a K step are read where they are
-        L.rq = ceil_div(r, kBK);
         L.part_bytes = std::min<size_t>(kPartBytes, (size_t)kXcds * kMaxParts * std::min(T, kTileM) * kTileN * 4);
         L.xk = take(L.copy ? (size_t)T * parts * L.nk * kBK * 2 : 0);
         L.v = take((size_t)L.stream.groups * T * r * 4);
-        L.vk = take((size_t)T * L.vparts * L.rq * kBK * 2);
-        L.list = take((size_t)ceil_div(T, 32) * (kTileM + 1) * 4);   // tiles of 32 tokens at least
         L.part = take(L.part_bytes);
     }
     L.bytes = at;
@@ -1066,10 +1099,6 @@ hipError_t launch_gemm(AdapterParams p, const AdapterPlan &L, uint8_t *ws, hipSt
     GemmParams g{};
     g.p = p;
     g.steps = p.w ? L.nk : 0;
-    g.vk = reinterpret_cast<uint16_t *>(ws + L.vk);
-    g.vparts = L.vparts;
-    g.rq = L.rq;
-    g.list = reinterpret_cast<int32_t *>(ws + L.list);
     g.ntiles = ceil_div(p.o, kTileN);
     g.slots = std::max(1, device_cu_count() / kXcds);
     const Cut cut = best_cut(p.T, parts, g.ntiles, g.steps, g.slots, L.part_bytes);
@@ -1077,10 +1106,11 @@ hipError_t launch_gemm(AdapterParams p, const AdapterPlan &L, uint8_t *ws, hipSt
     g.prows = std::min(p.T, ceil_div(ceil_div(p.T, 32), g.mtiles) * 32);
     g.maxparts = (int)std::min<size_t>(kMaxParts, L.part_bytes / ((size_t)kXcds * g.prows * kTileN * 4));
     g.part = reinterpret_cast<float *>(ws + L.part);
-    const int v_blocks = ceil_div((int64_t)p.T * L.rq * kBK, 256);
-    hipLaunchKernelGGL(k_adapter_parts, dim3((unsigned)(ceil_div(g.mtiles, 4) + v_blocks)), dim3(256), 0, s, g);
-    if ((e = hipGetLastError()) != hipSuccess) return e;
     const int U = g.mtiles * g.ntiles;
+    if (p.n > 0 && p.vgroups > 1) {
+        hipLaunchKernelGGL(k_adapter_join, dim3((unsigned)ceil_div((int64_t)p.T * p.r, 1024)), dim3(256), 0, s, p);
+        if ((e = hipGetLastError()) != hipSuccess) return e;
+    }
     bool tail = false;
     for (int x = 0; x < kXcds; ++x) {
         const int left = tile_plan(U, g.slots, x, 1).units % g.slots;   // (an XCD may have a tile less than the others)

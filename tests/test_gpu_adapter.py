@@ -255,6 +255,19 @@ def test_offsets_beyond_32_bits():
         assert torch.equal(c2.run(), y)
 
 
+@pytest.mark.parametrize("act", ACTS)
+@pytest.mark.parametrize("T,r,n,spread", [
+    (65536, 8, 3, "each"),     # the most tokens of a call
+    (65536, 8, 300, "runs"),
+    (300, 128, 40, "each"),    # more adapters in a tile than fit beside their v, twice 64 ranks
+    (300, 72, 40, "runs"),     # the second 64 ranks end early
+])
+def test_many_tokens_and_many_adapters(T, r, n, spread, act):
+    say(f"adapter {T} tokens r={r} n={n} {spread} {act}")
+    c = Case(torch_cuda(), 71 + T + n, T, 200, 296, r, n, act, spread=spread, y_in=True)
+    c.close(c.run(), f"{T} tokens, {n} adapters")
+
+
 def test_arguments():
     """Tensors the kernels could not read as they are refused by name; no tokens are no call."""
     torch = torch_cuda()
