@@ -597,15 +597,16 @@ __device__ __forceinline__ void wait_and_barrier()
 }
 
 // A tile of tokens row0 .. row0 + rows (up to HB * 32) by W rows nt * 256 ..: K steps k0 .. k0 +
-// nsteps, the adapters' steps too if `ext`. Two waves split the tokens and four the rows of W; both
-// operands go straight to LDS in rings of K steps, swizzled so that the operand reads touch all
-// banks evenly; one barrier per step (the same scheme as the experts' grouped products). Q: the
-// activations' parts; a step holds all of them, as Q * HB * 32 rows that share the sums, so that
-// a step of W is read once for them (with the parts as further K steps 333 tokens on 3592 x 2568 took
-// 81 us, 65 so).
+// nsteps, and every `parts`-th of the tile's adapters from the ks-th on (64 tokens with 64 adapters
+// of rank 128 on 4096 x 14336 took 183 us with all of them in the last part, 99 so). Two waves split
+// the tokens and four the rows of W; both operands go straight to LDS in rings of K steps,
+// swizzled so that the operand reads touch all banks evenly; one barrier per step (the same scheme
+// as the experts' grouped products). Q: the activations' parts; a step holds all of them, as
+// Q * HB * 32 rows that share the sums, so that a step of W is read once for them (with the parts as
+// further K steps 333 tokens on 3592 x 2568 took 81 us, 65 so).
 template <bool kOnce, int HB, int Q>
 __device__ __forceinline__ void project_tile(const GemmParams &g, uint8_t *lds, int row0, int rows, int nt, int mt, int k0,
-                                             int nsteps, int start, bool ext, float *part)
+                                             int nsteps, int start, int ks, int parts, float *part)
 {
     constexpr int EB = HB * Q;
     using C = TileCfg<EB>;
@@ -724,7 +725,7 @@ __device__ __forceinline__ void project_tile(const GemmParams &g, uint8_t *lds, 
         step(std::integral_constant<int, kFinal>{});
     }
 
-    if (ext) {
+    if (p.n > 0) {
         // The adapters: 64 ranks of the tile's v are put into LDS in bf16 parts, as token rows of a K
         // step, and the B rows of as many adapters as fit beside them. Every token's v meets every
         // adapter of the tile; the products are added to the tokens of that adapter only (not by
@@ -743,7 +744,10 @@ __device__ __forceinline__ void project_tile(const GemmParams &g, uint8_t *lds, 
         auto adapter = [&](int u) { return u == 0 ? a[0] : u == 1 ? a[1] : u == 2 ? a[2] : a[kRound - 1]; };
         auto next_round = [&](int rc) {   // false: there is none
 #pragma unroll
-            for (int u = 0; u < kRound; ++u) a[u] = take_adapter(left);
+            for (int u = 0; u < kRound; ++u) {
+                a[u] = take_adapter(left);
+                for (int i = 1; i < parts; ++i) (void)take_adapter(left);
+            }
             if (a[0] < 0) return false;
             wait_and_barrier<0>();        // what LDS holds is read
 #pragma unroll 1
@@ -759,6 +763,7 @@ __device__ __forceinline__ void project_tile(const GemmParams &g, uint8_t *lds, 
         for (int rc = 0; rc * kBK < p.r; ++rc) {
 #pragma unroll
             for (int k = 0; k < kIds; ++k) left[k] = id[k];
+            for (int i = 0; i < ks; ++i) (void)take_adapter(left);
             if (!next_round(rc)) break;
 #pragma unroll 1
             for (int i = threadIdx.x; i < HB * 32 * (kBK / 8); i += kThreads) {
@@ -866,10 +871,9 @@ __global__ __launch_bounds__(kThreads) void k_adapter_gemm(GemmParams g)
         const int row0 = first_row(g.p.T, g.mtiles, mt), rows = first_row(g.p.T, g.mtiles, mt + 1) - row0;
         const int k0 = (int)((int64_t)g.steps * ks / parts), kn = (int)((int64_t)g.steps * (ks + 1) / parts) - k0;
         const int start = g.mtiles == 1 && kn > 0 ? (int)((unsigned)(nt * kStagger) % (unsigned)kn) : 0;
-        const bool ext = ks == parts - 1;
         switch ((rows + 31) >> 5) {
 #define MOE_HB_CASE(N) \
-    case N: if constexpr (N <= tile_blocks(Q)) project_tile<kOnce, N, Q>(g, lds, row0, rows, nt, mt, k0, kn, start, ext, part); break;
+    case N: if constexpr (N <= tile_blocks(Q)) project_tile<kOnce, N, Q>(g, lds, row0, rows, nt, mt, k0, kn, start, ks, parts, part); break;
             MOE_HB_CASE(1) MOE_HB_CASE(2) MOE_HB_CASE(3) MOE_HB_CASE(4)
             MOE_HB_CASE(5) MOE_HB_CASE(6) MOE_HB_CASE(7) MOE_HB_CASE(8)
 #undef MOE_HB_CASE

@@ -110,7 +110,7 @@ def test_decode_batches(T, d, o, r, n, spread, act):
 @pytest.mark.parametrize("T,d,o,r,n,spread", [
     (17, 8, 8, 8, 2, "each"),            # least of everything
     (17, 4096, 264, 16, 30, "each"),     # one block of 32 rows, split over K
-    (40, 2056, 136, 32, 9, "each"),      # 33 to 48 tokens: a shrink block of four column blocks
+    (40, 2056, 136, 32, 9, "each"),      # the last 16 tokens begin among the ones before
     (64, 264, 520, 24, 7, "runs"),       # padded K steps
     (97, 1024, 2048, 128, 3, "each"),    # two K steps of ranks
     (160, 576, 776, 64, 5, "runs"),
