@@ -935,8 +935,8 @@ StreamPlan stream_plan(int d, int nb)
 // Shrink: blocks as large as leave some work for most of the chip (a block's adapters' rows of A are
 // read once for it), then units as long. (512 tokens of 4096 values, 8 adapters of rank 32: 35 us in
 // blocks of 128 tokens and units of 8 chunks, 9.5 in blocks of 32 and units of one; 4096 tokens of
-// 14336 values, 16 of rank 64: 67 us in blocks of 128 and units of 4 chunks, some 20 more with blocks of
-// 64 or units of 3.)
+// 14336 values, 16 of rank 64: 64 us in blocks of 128 and units of 4 chunks, some 20 more with blocks of
+// 64 or units of 3, the same with units of 6.)
 StreamPlan shrink_plan(int T, int d, int r, int *tb)
 {
     StreamPlan best{};
