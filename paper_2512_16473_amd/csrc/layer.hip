@@ -4,7 +4,8 @@
 //   FFN(x) = W2 (SiLU(W1 x) * W3 x)
 //
 // Every selected expert's weights are read once for all the tokens. Kernels, on one stream:
-//   1. prepare: the logits in fp64, and x as operand columns;
+//   1. prepare: the logits in fp64, and x as operand columns (the smallest calls leave it out, and
+//      each work group of gate/up does this for itself);
 //   2. gate/up: each work group selects the top k from the logits and then takes blocks of 8
 //      rows of W1 and the same 8 of W3, of the shared expert and of the selected ones. All the
 //      tokens are multiplied with every expert's rows (the matrix cores have room for 16 columns
@@ -40,6 +41,7 @@ struct LayerParams {
     const uint8_t *shared;        // shared expert's slab or null
     const int32_t *slotmap;       // [n] or null (expert e in slot e)
     int T, d, f, fs, n, k, nslots;
+    bool alone;                   // gate/up computes logits and columns itself
     double *logits;               // [T][n]
     int32_t *idx;                 // [T][k]
     float *w;                     // [T][k]
@@ -92,6 +94,53 @@ __device__ __forceinline__ void build_jobs(const LayerParams &p, Jobs &J)
     __syncthreads();
 }
 
+// 16 bytes of x as columns: 8 values of a token's part.
+__device__ __forceinline__ uint4 x_column(const LayerParams &p, int i)
+{
+    const int cols = p.T * x_parts(p.bf16);
+    const int c = i % cols, k = i / cols * 8, q = c / p.T, t = c - q * p.T;
+    if (k >= p.d) return make_uint4(0, 0, 0, 0);
+    if (p.bf16) return *reinterpret_cast<const uint4 *>(static_cast<const uint16_t *>(p.x) + (size_t)t * p.d + k);
+    const float4 *v = reinterpret_cast<const float4 *>(static_cast<const float *>(p.x) + (size_t)t * p.d + k);
+    const float4 a = v[0], b = v[1];
+    const float f[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+    uint32_t u[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) u[j] = part_of<3>(f[2 * j], q) | ((uint32_t)part_of<3>(f[2 * j + 1], q) << 16);
+    return make_uint4(u[0], u[1], u[2], u[3]);
+}
+__host__ __device__ inline int x_column_pieces(const LayerParams &p) { return chunks_of(p.d) * (kChunk / 8) * p.T * x_parts(p.bf16); }
+
+// A wave's logit of expert e for token t, of every `split`-th 256 values from the part-th on.
+__device__ __forceinline__ double logit(const LayerParams &p, int e, int t, int part, int split)
+{
+    double acc = 0.0;
+    const float4 *w = reinterpret_cast<const float4 *>(p.wr + (size_t)e * p.d);
+    const int nq = p.d >> 2, c0 = part * kWave + (threadIdx.x & 63), step = split * kWave;
+    auto dot = [&](const float4 a, const float4 b) {
+        acc = fma((double)a.x, (double)b.x, acc);
+        acc = fma((double)a.y, (double)b.y, acc);
+        acc = fma((double)a.z, (double)b.z, acc);
+        acc = fma((double)a.w, (double)b.w, acc);
+    };
+    if (p.bf16) {
+        const uint2 *x = reinterpret_cast<const uint2 *>(static_cast<const uint16_t *>(p.x) + (size_t)t * p.d);
+#pragma unroll 8
+        for (int c = c0; c < nq; c += step) {
+            const uint2 v = x[c];
+            dot(w[c], make_float4(__uint_as_float(v.x << 16), __uint_as_float(v.x & 0xffff0000u),
+                                  __uint_as_float(v.y << 16), __uint_as_float(v.y & 0xffff0000u)));
+        }
+    } else {
+        const float4 *x = reinterpret_cast<const float4 *>(static_cast<const float *>(p.x) + (size_t)t * p.d);
+#pragma unroll 8
+        for (int c = c0; c < nq; c += step) dot(w[c], x[c]);
+    }
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) acc += __shfl_xor(acc, o, kWave);
+    return acc;
+}
+
 // Blocks of the first `logit_blocks`: logits. A wave sums a `split`-th of an (expert, token) row; the
 // work group adds up (four waves: 4 / split rows). Row i is expert i / T and token i % T. The other
 // blocks: x as columns, 8 values of a token and part per thread; and the row counts cleared.
@@ -100,53 +149,14 @@ __global__ __launch_bounds__(256) void k_layer_prepare(LayerParams p, int split,
     __shared__ double part[4];
     if ((int)blockIdx.x >= logit_blocks) {
         const int i = (blockIdx.x - logit_blocks) * 256 + threadIdx.x;
-        const int parts = x_parts(p.bf16), cols = p.T * parts;
         if (i < (p.d + kRows - 1) / kRows) p.counts[i] = 0;
-        if (i >= chunks_of(p.d) * (kChunk / 8) * cols) return;
-        const int c = i % cols, k = i / cols * 8, q = c / p.T, t = c - q * p.T;
-        uint4 o = make_uint4(0, 0, 0, 0);
-        if (k < p.d && p.bf16) {
-            o = *reinterpret_cast<const uint4 *>(static_cast<const uint16_t *>(p.x) + (size_t)t * p.d + k);
-        } else if (k < p.d) {
-            const float *v = static_cast<const float *>(p.x) + (size_t)t * p.d + k;
-            uint32_t u[4];
-#pragma unroll
-            for (int j = 0; j < 4; ++j) u[j] = part_of<3>(v[2 * j], q) | ((uint32_t)part_of<3>(v[2 * j + 1], q) << 16);
-            o = make_uint4(u[0], u[1], u[2], u[3]);
-        }
-        *reinterpret_cast<uint4 *>(p.xc + (size_t)i * 16) = o;
+        if (i < x_column_pieces(p)) *reinterpret_cast<uint4 *>(p.xc + (size_t)i * 16) = x_column(p, i);
         return;
     }
     const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6;
     const int i = blockIdx.x * (4 / split) + wv / split;
-    double acc = 0.0;
     const int e = i / p.T, t = i - e * p.T;
-    if (i < p.n * p.T) {
-        const float4 *w = reinterpret_cast<const float4 *>(p.wr + (size_t)e * p.d);
-        const int nq = p.d >> 2, step = split * kWave;
-        auto dot = [&](const float4 a, const float4 b) {
-            acc = fma((double)a.x, (double)b.x, acc);
-            acc = fma((double)a.y, (double)b.y, acc);
-            acc = fma((double)a.z, (double)b.z, acc);
-            acc = fma((double)a.w, (double)b.w, acc);
-        };
-        const int c0 = (wv % split) * kWave + lane;
-        if (p.bf16) {
-            const uint2 *x = reinterpret_cast<const uint2 *>(static_cast<const uint16_t *>(p.x) + (size_t)t * p.d);
-#pragma unroll 8
-            for (int c = c0; c < nq; c += step) {
-                const uint2 v = x[c];
-                dot(w[c], make_float4(__uint_as_float(v.x << 16), __uint_as_float(v.x & 0xffff0000u),
-                                      __uint_as_float(v.y << 16), __uint_as_float(v.y & 0xffff0000u)));
-            }
-        } else {
-            const float4 *x = reinterpret_cast<const float4 *>(static_cast<const float *>(p.x) + (size_t)t * p.d);
-#pragma unroll 8
-            for (int c = c0; c < nq; c += step) dot(w[c], x[c]);
-        }
-    }
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) acc += __shfl_xor(acc, o, kWave);
+    double acc = i < p.n * p.T ? logit(p, e, t, wv % split, split) : 0.0;
     if (lane == 0) part[wv] = acc;
     __syncthreads();
     if (lane == 0 && wv % split == 0 && i < p.n * p.T) {
@@ -163,6 +173,22 @@ __device__ __forceinline__ void load_logits(const LayerParams &p, double *lg, Jo
         lg[i] = v != v ? -INFINITY : v;
     }
     if (threadIdx.x < MOE_MAX_EXPERTS) J.users[threadIdx.x] = 0;
+}
+// The same without the first kernel: this work group computes the logits, and x's columns into `xc`
+// (LDS). Block 0 clears the row counts, which only the next kernel uses.
+__device__ __forceinline__ void own_logits(const LayerParams &p, double *lg, Jobs &J, uint8_t *xc)
+{
+    const int tid = threadIdx.x, wv = __builtin_amdgcn_readfirstlane(tid >> 6);
+    if (blockIdx.x == 0)
+        for (int i = tid; i < (p.d + kRows - 1) / kRows; i += kThreads) p.counts[i] = 0;
+    for (int i = tid; i < x_column_pieces(p); i += kThreads) *reinterpret_cast<uint4 *>(xc + i * 16) = x_column(p, i);
+    for (int i = wv; i < p.n * p.T; i += kWaves) {
+        const int e = i / p.T, t = i - e * p.T;
+        const double v = logit(p, e, t, 0, 1);
+        if ((tid & 63) == 0) lg[t * p.n + e] = v != v ? -INFINITY : v;
+    }
+    if (tid < MOE_MAX_EXPERTS) J.users[tid] = 0;
+    __syncthreads();
 }
 // Gate weight of token t for job j (zero: did not select it), from the selection.
 __device__ __forceinline__ void gate_table(const LayerParams &p, const int *sel, const float *w, const Jobs &J, float *table)
@@ -286,9 +312,17 @@ __global__ __launch_bounds__(kThreads) void k_layer_gate_up(LayerParams p)
     src.r.lane_row = lane_row_of(src.r.bytes);
     const int cnt = src.cnt;
     bf16x8_t bx[S][2][NB];
-    load_columns<S, NB, STK>(p.xc + (size_t)src.r.c0 * (kChunk / 8) * xcols * 16, xcols, p.T, cnt, bx);
-    load_logits(p, lg, J);
-    settle(bx);
+    const size_t x_at = (size_t)src.r.c0 * (kChunk / 8) * xcols * 16;
+    if (NB == 1 && p.alone) {
+        own_logits(p, lg, J, lds);
+        load_columns<S, NB, STK>(lds + x_at, xcols, p.T, cnt, bx);
+        settle(bx);
+        __syncthreads();   // the ring may be filled
+    } else {
+        load_columns<S, NB, STK>(p.xc + x_at, xcols, p.T, cnt, bx);
+        load_logits(p, lg, J);
+        settle(bx);
+    }
     // Where the shared expert fills the ring, it does so while the routing is worked out. (The items
     // that start() looks at are all its own.)
     Stream_t st;
@@ -539,17 +573,27 @@ hipError_t launch_down(const LayerParams &p, int groups, hipStream_t s)
     return hipGetLastError();
 }
 
-hipError_t launch_layer(const LayerParams &p, const LayerPlan &L, hipStream_t s)
+hipError_t launch_layer(LayerParams p, const LayerPlan &L, hipStream_t s)
 {
     (void)hipGetLastError();
     hipError_t e;
-    // one wave per row where there are enough of them, else four
-    const int split = p.n * p.T <= 4 * device_cu_count() ? 4 : 1;
-    const int logit_blocks = ceil_div(p.n * p.T, 4 / split);
-    const int column_blocks_x = ceil_div(chunks_of(p.d) * (kChunk / 8) * p.T * x_parts(p.bf16), 256);
-    hipLaunchKernelGGL(k_layer_prepare, dim3((unsigned)(logit_blocks + column_blocks_x)), dim3(256), 0, s, p, split, logit_blocks);
-    if ((e = hipGetLastError()) != hipSuccess) return e;
     const int nb1 = column_blocks(x_parts(p.bf16), p.T), s1 = ceil_div(chunks_of(p.d), kWaves);
+    // The smallest calls are bound by their launches: with a logit for each wave of a work group at
+    // most, gate/up computes them itself, 256 x 512, 4 experts, one token: 18.2 us through Python and
+    // 14.9 in a graph with the first kernel, 14.7 and 14.0 without; 2048 x 1024, 8 experts: 18.1 and
+    // 19.1, 17.6 and 19.2. Longer rows take longer so (4096: 21.9 and 20.4, 21.9 and 21.1; a Mixtral-
+    // shaped layer 121 us, 123 without), and so do more of them (512 x 512, 8 experts, 4 tokens: 17.7
+    // and 16.4, 19.1 and 18.5).
+    p.alone = p.n * p.T <= kWaves && p.d <= 2048 && nb1 == 1 &&
+              x_column_pieces(p) * 16 <= kWaves * ring_stages(s1) * kStageBytes;
+    if (!p.alone) {
+        // one wave per row where there are enough of them, else four
+        const int split = p.n * p.T <= 4 * device_cu_count() ? 4 : 1;
+        const int logit_blocks = ceil_div(p.n * p.T, 4 / split);
+        const int column_blocks_x = ceil_div(x_column_pieces(p), 256);
+        hipLaunchKernelGGL(k_layer_prepare, dim3((unsigned)(logit_blocks + column_blocks_x)), dim3(256), 0, s, p, split, logit_blocks);
+        if ((e = hipGetLastError()) != hipSuccess) return e;
+    }
     // T * d <= MOE_LAYER_MAX_VALUES: 16 chunks a wave with one column block, 11 with two, 6 with three
     switch (nb1 * 100 + s1) {
 #define MOE_GU(NB, S) \

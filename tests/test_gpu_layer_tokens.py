@@ -137,6 +137,41 @@ def test_layer_against_its_definition(d, f, n, k, fs, T, act):
     check(layer, states(torch, T + 100, T, d, dtype), states(torch, 5, T, d, dtype), "with y_in")
 
 
+@pytest.mark.parametrize("act", ["float32", "bfloat16"])
+@pytest.mark.parametrize("d,f,n,k,fs,T", [
+    # up to 8 logits and rows of 2048: routed inside gate/up
+    (2048, 264, 8, 2, 0, 1),
+    (2040, 72, 4, 4, 0, 2),          # ends inside a chunk
+    (1544, 136, 2, 1, 0, 4),         # rows of four chunks a wave, the last waves short
+    (1536, 136, 1, 1, 24, 5),        # the columns fill the rings; one expert
+    (520, 64, 1, 1, 16, 8),          # bf16: eight columns; fp32: two column blocks
+    (256, 4104, 3, 2, 40960, 1),     # a shared expert that fills the rings before the routing
+    (2056, 264, 8, 2, 0, 1),         # just beyond
+    (512, 264, 9, 2, 0, 1),
+])
+def test_the_smallest_calls(d, f, n, k, fs, T, act):
+    torch = torch_cuda()
+    say("layer_tokens small", d, f, n, k, fs, T, act)
+    layer = Layer(torch, d * 5 + f + T, d, f, n, k, fs)
+    dtype = getattr(torch, act)
+    check(layer, states(torch, T, T, d, dtype), states(torch, 5, T, d, dtype), "with y_in")
+    x = states(torch, T + 9, T, d, dtype)
+    x[0, d // 2] = float("nan")
+    y, _, _ = layer.run(x)
+    assert torch.isnan(y[0]).all()
+    clean = x.clone()
+    clean[0, d // 2] = 0.0
+    ref, _, _ = layer.run(clean)
+    if T > 1:
+        got, want = y[1:].double(), ref[1:].double()
+        rms = want.pow(2).mean(1, keepdim=True).sqrt()
+        # the batch's experts, and with them the groups of the sums, may differ
+        tol = 16 * 2.0 ** -24 * (2 * d ** 0.5 + (k * f + fs) ** 0.5) * rms
+        if act == "bfloat16":
+            tol = tol + 2.0 ** -16 * 8 * rms + 2.0 ** -7 * want.abs()
+        assert bool(((got - want).abs() <= tol).all())
+
+
 def test_full_mixtral_layer():
     torch = torch_cuda()
     say("layer_tokens mixtral")
@@ -237,13 +272,14 @@ def test_large_and_small_values():
         check(layer, x * scale, None, f"scale {scale}")
 
 
-def test_captured_and_replayed():
+@pytest.mark.parametrize("T,n", [(4, 8), (1, 8)])   # three launches, and two
+def test_captured_and_replayed(T, n):
     """The call in a graph, replayed between eager calls on the same workspace's twin."""
     torch = torch_cuda()
     say("layer_tokens graph")
-    layer = Layer(torch, 15, 512, 520, 8, 2, 136)
-    x = states(torch, 8, 4, 512, torch.float32)
-    y, ws = torch.empty_like(x), layer.workspace(4)
+    layer = Layer(torch, 15, 512, 520, n, 2, 136)
+    x = states(torch, 8, T, 512, torch.float32)
+    y, ws = torch.empty_like(x), layer.workspace(T)
     side = torch.cuda.Stream()
     side.wait_stream(torch.cuda.current_stream())
     with torch.cuda.stream(side):
@@ -253,7 +289,7 @@ def test_captured_and_replayed():
     with torch.cuda.graph(graph):
         layer.call(x, y, ws)
     for i in range(4):
-        x.copy_(states(torch, 20 + i, 4, 512, torch.float32))
+        x.copy_(states(torch, 20 + i, T, 512, torch.float32))
         graph.replay()
         eager, _, _ = layer.run(x)
         torch.cuda.synchronize()
