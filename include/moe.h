@@ -261,8 +261,8 @@ typedef struct moe_tokens_desc {
  * selected it, and the shared expert's once. An expert whose slot is outside [0, n_slots)
  * contributes nothing (its share is the caller's, who finds it in idx and w; a negative slot is
  * the table's "not cached").
- * x, y_in, y   device [T][d] of act_type (MOE_F32 or MOE_BF16); y_in may be NULL (zero) or y
- *              itself. fp32 activations enter the products exactly (three bf16 parts), hidden
+ * x, y_in, y   device [T][d] of act_type (MOE_F32 or MOE_BF16); y_in may be NULL (zero), x or y
+ *              itself, and y may be x. fp32 activations enter the products exactly (three bf16 parts), hidden
  *              values of a bf16 layer as two bf16 parts; sums are fp32, a bf16 y is rounded once.
  * idx, w       device int32 / fp32 [T][k], the routing as moe_router_topk gives it; may be NULL
  * workspace    device, 256-byte aligned, >= moe_layer_tokens_workspace_bytes(T, d, f, n, k,
@@ -293,7 +293,7 @@ typedef struct moe_adapter_desc {
  * Any order of tokens is right; those of one adapter side by side are fastest.
  * x, y_in, y   device, rows of d_in / d_out values of act_type (MOE_F32 or MOE_BF16), row strides
  *              in elements (multiples of 8, at most MOE_ADAPTER_MAX_STRIDE); y_in may be NULL
- *              (zero) or y itself, x must not overlap y. fp32 activations enter the products
+ *              (zero), x or y itself, x must not overlap y. fp32 activations enter the products
  *              exactly (three bf16 parts, so beyond 16 tokens an fp32 call does three times a
  *              bf16 call's matrix work); sums are fp32, a bf16 y is rounded once.
  * adapters     device int32 [T]

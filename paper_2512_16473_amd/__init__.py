@@ -254,6 +254,11 @@ def layer_tokens_workspace_bytes(T, d, f, n, k, f_shared=0) -> int:
     return int(_lib.moe_layer_tokens_workspace_bytes(T, d, f, n, k, f_shared))
 
 
+def _room(t):
+    """Address and bytes of a workspace (None: no tokens need none)."""
+    return (0, 0) if t is None else (t.data_ptr(), t.nbytes)
+
+
 def layer_tokens(x, w_router, slot_pool, f, k, y, workspace, n_slots=None, slotmap=None, shared=None, f_shared=0,
                  y_in=None, idx=None, w=None, stream=None):
     """y[t] = y_in[t] + the routed experts' output for x[t] (+ the shared expert's), the whole
@@ -279,7 +284,7 @@ def layer_tokens(x, w_router, slot_pool, f, k, y, workspace, n_slots=None, slotm
     _want_bytes(fn, "workspace", workspace, int(T > 0), device)
     P = TokensDesc(d, f, n, k, f_shared, n_slots, w_router.data_ptr(), _addr(slot_pool), _addr(slotmap), _addr(shared))
     _on(device, "moe_layer_tokens", _lib.moe_layer_tokens, ctypes.byref(P), x.data_ptr(), T, _addr(y_in), y.data_ptr(),
-        _addr(idx), _addr(w), act, workspace.data_ptr(), workspace.nbytes, stream=stream)
+        _addr(idx), _addr(w), act, *_room(workspace), stream=stream)
     return y
 
 
@@ -325,7 +330,7 @@ def adapter_project(x, w, a, b, adapters, y, workspace, scale=None, y_in=None, s
     P = AdapterDesc(d_in, d_out, n, rank, _addr(w), a.data_ptr(), b.data_ptr(), _addr(scale))
     _on(device, "moe_adapter_project", _lib.moe_adapter_project, ctypes.byref(P), x.data_ptr(), _row_stride(x), T,
         adapters.data_ptr(), _addr(y_in), 0 if y_in is None else _row_stride(y_in), y.data_ptr(), _row_stride(y), act,
-        workspace.data_ptr(), workspace.nbytes, stream=stream)
+        *_room(workspace), stream=stream)
     return y
 
 

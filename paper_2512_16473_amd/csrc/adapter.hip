@@ -1183,6 +1183,7 @@ int moe_adapter_project(const moe_adapter_desc *P, const void *x, int64_t x_stri
     const bool bf16 = act_type == MOE_BF16;
     const moe::AdapterPlan L = moe::plan_adapter(T, P->d_in, P->d_out, P->rank, bf16);
     MOE_REQUIRE(workspace_bytes >= L.bytes, "moe_adapter_project: workspace %zu < %zu bytes", workspace_bytes, L.bytes);
+    MOE_REQUIRE(x != y, "moe_adapter_project: y over x, which is read after y's first rows are written");
     moe::AdapterParams p{};
     p.x = x;
     p.bf16 = bf16;

@@ -485,6 +485,7 @@ def _adapter_call(T=2, d=64, o=64, n=4, r=8, act=0, ws=256, nbytes=1 << 40, x=25
     (dict(y_in=512, yis=32), b"y_in_stride=32"), (dict(y_in=512, yis=(1 << 26) + 8), b"y_in_stride=67108872"), (dict(y_in=256, yis=72), b"another stride"), (dict(x=264), b"16-byte aligned"),
     (dict(y=264), b"16-byte aligned"), (dict(w=8), b"16-byte aligned"), (dict(a=8), b"16-byte aligned"),
     (dict(b=8), b"16-byte aligned"), (dict(ws=128), b"256-byte aligned"), (dict(nbytes=0), b"workspace 0 <"),
+    (dict(x=512, y=512), b"y over x"),
 ])
 def test_adapter_refusals(bad, message):
     assert _adapter_call(**bad) == _abi.MOE_EINVAL

@@ -290,6 +290,7 @@ def test_arguments():
         moe.adapter_project(**{**good, "workspace": good["workspace"][:256]})
     none = torch.empty((0, 64), dtype=torch.bfloat16, device="cuda")
     moe.adapter_project(none, c.w, c.a, c.b, c.ids[:0], y[:0], good["workspace"][:0])
+    moe.adapter_project(none, c.w, c.a, c.b, c.ids[:0], y[:0], None)
 
 
 def test_a_batch_through_the_layer_and_its_adapted_shared_expert():

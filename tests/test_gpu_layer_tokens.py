@@ -214,6 +214,22 @@ def test_in_place_and_neighbours():
     assert torch.equal(buf[:5], y) and torch.all(buf[5:] == 123.0)
 
 
+@pytest.mark.parametrize("act", ["float32", "bfloat16"])
+@pytest.mark.parametrize("d,n,T,fs", [(264, 6, 5, 72), (1024, 4, 2, 0), (4096, 8, 8, 0), (256, 2, 1, 2056)])
+def test_residual_over_its_own_input(d, n, T, fs, act):
+    """x as y_in, and y over both: a residual layer that keeps its states in one buffer."""
+    torch = torch_cuda()
+    say("layer_tokens over x", d, n, T, fs, act)
+    layer = Layer(torch, 30 + d, d, 520, n, 2, fs)
+    x = states(torch, 3, T, d, getattr(torch, act))
+    y, _, _ = layer.run(x, x)
+    state = x.clone()
+    for _ in range(3):
+        state.copy_(x)
+        layer.call(state, state, layer.workspace(T), y_in=state)
+        assert torch.equal(state, y)
+
+
 def test_ties_and_a_token_of_nan():
     """Equal logits go to the lower ids; a token of NaN or infinities leaves the others alone."""
     torch = torch_cuda()
