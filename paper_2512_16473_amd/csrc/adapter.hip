@@ -598,7 +598,7 @@ __device__ __forceinline__ void wait_and_barrier()
 
 // A tile of tokens row0 .. row0 + rows (up to HB * 32) by W rows nt * 256 ..: K steps k0 .. k0 +
 // nsteps, and every `parts`-th of the tile's adapters from the ks-th on (64 tokens with 64 adapters
-// of rank 128 on 4096 x 14336 took 183 us with all of them in the last part, 99 so). Two waves split
+// of rank 128 on 4096 x 14336 took twice as long with all of them in the last part). Two waves split
 // the tokens and four the rows of W; both operands go straight to LDS in rings of K steps,
 // swizzled so that the operand reads touch all banks evenly; one barrier per step (the same scheme
 // as the experts' grouped products). Q: the activations' parts; a step holds all of them, as
@@ -729,42 +729,46 @@ __device__ __forceinline__ void project_tile(const GemmParams &g, uint8_t *lds, 
         // The adapters: 64 ranks of the tile's v are put into LDS in bf16 parts, as token rows of a K
         // step, and the B rows of as many adapters as fit beside them. Every token's v meets every
         // adapter of the tile; the products are added to the tokens of that adapter only (not by
-        // zeros in v: one request's infinite or NaN weights must not reach another's tokens). (With
-        // v's parts made by a kernel of their own and loaded again for each adapter, 512 tokens of 9
-        // runs on 4096 x 14336 took 90 us, 86 so; 333 in fp32 on 3592 x 2568 64 and 57.)
+        // zeros in v: one request's infinite or NaN weights must not reach another's tokens), and
+        // blocks of 16 tokens without it are passed over (64 tokens with 64 adapters of rank 128 on
+        // 4096 x 14336: 94 us without that, 78 with; 4096 with 16, scattered: 1045 and 934). (With v's
+        // parts made by a kernel of their own and loaded again for each adapter, 512 tokens of 9 runs on
+        // 4096 x 14336 took 90 us, 84 so; 333 in fp32 on 3592 x 2568 64 and 57.)
         constexpr int VP = Q == 1 ? 2 : 3, kVBytes = HB * 32 * kRowBytes, kFit = (kLdsBytes - VP * kVBytes) / kBBytes;
-        constexpr int kRound = kFit < 4 ? kFit : 4, kIds = (HB * 32 + kWave - 1) / kWave;
+        constexpr int kRing = kFit < 4 ? kFit : 4, kIds = (HB * 32 + kWave - 1) / kWave;
         uint8_t *const bst = lds + VP * kVBytes;
         int id[kIds], own[HB];
         load_ids(p, row0, rows, id);
 #pragma unroll
         for (int m = 0; m < HB; ++m) own[m] = p.ids[row0 + min((wm * HB + m) * 16 + (lane & 15), rows - 1)];
         const int r2 = p.r * 2;
-        int left[kIds], a[kRound];
-        auto adapter = [&](int u) { return u == 0 ? a[0] : u == 1 ? a[1] : u == 2 ? a[2] : a[kRound - 1]; };
-        auto next_round = [&](int rc) {   // false: there is none
+        int left[kIds];
+        auto mine = [&]() {                  // this part's next adapter, -1: none
+            const int a = take_adapter(left);
+            for (int i = 1; i < parts && a >= 0; ++i) (void)take_adapter(left);
+            return a;
+        };
+        auto load = [&](int a, int rc, int stage) {
 #pragma unroll
-            for (int u = 0; u < kRound; ++u) {
-                a[u] = take_adapter(left);
-                for (int i = 1; i < parts; ++i) (void)take_adapter(left);
-            }
-            if (a[0] < 0) return false;
-            wait_and_barrier<0>();        // what LDS holds is read
-#pragma unroll 1
-            for (int u = 0; u < kRound && adapter(u) >= 0; ++u) {
-#pragma unroll
-                for (int i = 0; i < kBLoads; ++i)   // (past the ranks v is zero)
-                    put_b(i, p.b + ((size_t)adapter(u) * p.o + w_block(i)) * r2 + (uint32_t)(lr * r2 + min(rc * kRowBytes + lc, r2 - 16)),
-                          bst + u * kBBytes);
-            }
-            return true;
+            for (int i = 0; i < kBLoads; ++i)   // (past the ranks v is zero)
+                put_b(i, p.b + ((size_t)a * p.o + w_block(i)) * r2 + (uint32_t)(lr * r2 + min(rc * kRowBytes + lc, r2 - 16)),
+                      bst + stage * kBBytes);
         };
 #pragma unroll 1
         for (int rc = 0; rc * kBK < p.r; ++rc) {
 #pragma unroll
             for (int k = 0; k < kIds; ++k) left[k] = id[k];
             for (int i = 0; i < ks; ++i) (void)take_adapter(left);
-            if (!next_round(rc)) break;
+            // a ring of B stages: the adapter that is multiplied, those behind it on their way
+            int now = mine(), next[kRing - 1];
+            if (now < 0) break;
+            wait_and_barrier<0>();   // what LDS holds is read
+            load(now, rc, 0);
+#pragma unroll
+            for (int u = 0; u < kRing - 2; ++u) {
+                next[u] = mine();
+                if (next[u] >= 0) load(next[u], rc, u + 1);
+            }
 #pragma unroll 1
             for (int i = threadIdx.x; i < HB * 32 * (kBK / 8); i += kThreads) {
                 const int tr = i / (kBK / 8), c = i % (kBK / 8);
@@ -778,72 +782,103 @@ __device__ __forceinline__ void project_tile(const GemmParams &g, uint8_t *lds, 
                     *reinterpret_cast<uint4 *>(lds + q * kVBytes + tr * kRowBytes + (c ^ (tr & 7)) * 16) = make_uint4(w[0], w[1], w[2], w[3]);
                 }
             }
+            int at = 0;
 #pragma unroll 1
             do {
-                wait_and_barrier<0>();
-#pragma unroll 1
-                for (int u = 0; u < kRound && adapter(u) >= 0; ++u) {
-                    const int now = adapter(u);
-                    asm volatile("" ::: "memory");   // v is read anew: held for the next adapter it would not fit the registers
-                    bf16x8_t w[2][4];
+                // the stage is here, and the one before is read by all
+                if (next[kRing - 3] >= 0) wait_and_barrier<(kRing - 2) * kBLoads>();
+                else wait_and_barrier<0>();
+                const int free = at == 0 ? kRing - 1 : at - 1;
+                next[kRing - 2] = next[kRing - 3] >= 0 ? mine() : -1;
+                if (next[kRing - 2] >= 0) load(next[kRing - 2], rc, free);
+                bf16x8_t w[2][4];
 #pragma unroll
-                    for (int kb = 0; kb < 2; ++kb)
+                for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
-                        for (int nb = 0; nb < 4; ++nb)
-                            w[kb][nb] = *reinterpret_cast<const bf16x8_t *>(bst + u * kBBytes + (wn * 64 + nb * 16) * kRowBytes + (rd ^ (kb * 64)));
+                    for (int nb = 0; nb < 4; ++nb)
+                        w[kb][nb] = *reinterpret_cast<const bf16x8_t *>(bst + at * kBBytes + (wn * 64 + nb * 16) * kRowBytes + (rd ^ (kb * 64)));
 #pragma unroll
-                    for (int m = 0; m < HB; ++m) {
-                        floatx4_t d[4];
+                for (int m = 0; m < HB; ++m) {
+                    if (__ballot(own[m] == now) == 0) continue;   // none of the 16 tokens
+                    floatx4_t d[4];
 #pragma unroll
-                        for (int nb = 0; nb < 4; ++nb) d[nb] = floatx4_t{0.f, 0.f, 0.f, 0.f};
+                    for (int nb = 0; nb < 4; ++nb) d[nb] = floatx4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                        for (int q = 0; q < VP; ++q)
+                    for (int q = 0; q < VP; ++q)
 #pragma unroll
-                            for (int kb = 0; kb < 2; ++kb) {
-                                const bf16x8_t v = *reinterpret_cast<const bf16x8_t *>(ra + q * kVBytes + m * 16 * kRowBytes + (rd ^ (kb * 64)));
+                        for (int kb = 0; kb < 2; ++kb) {
+                            const bf16x8_t v = *reinterpret_cast<const bf16x8_t *>(ra + q * kVBytes + m * 16 * kRowBytes + (rd ^ (kb * 64)));
 #pragma unroll
-                                for (int nb = 0; nb < 4; ++nb) d[nb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w[kb][nb], v, d[nb], 0, 0, 0);
-                            }
+                            for (int nb = 0; nb < 4; ++nb) d[nb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w[kb][nb], v, d[nb], 0, 0, 0);
+                        }
 #pragma unroll
-                        for (int nb = 0; nb < 4; ++nb)
+                    for (int nb = 0; nb < 4; ++nb)
 #pragma unroll
-                            for (int c = 0; c < 4; ++c) acc[m][nb][c] += own[m] == now ? d[nb][c] : 0.f;
-                        __builtin_amdgcn_sched_barrier(0);   // (not all the reads first)
-                    }
+                        for (int c = 0; c < 4; ++c) acc[m][nb][c] += own[m] == now ? d[nb][c] : 0.f;
+                    __builtin_amdgcn_sched_barrier(0);   // (not all the reads first)
                 }
-            } while (next_round(rc));
+                now = next[0];
+#pragma unroll
+                for (int u = 0; u + 1 < kRing - 1; ++u) next[u] = next[u + 1];
+                at = at + 1 == kRing ? 0 : at + 1;
+            } while (now >= 0);
         }
     }
 
     // result r of a 16x16 block: row 4 (lane / 16) + r of W, token lane % 16
-    const int c4 = 4 * (lane >> 4);
+    typedef __bf16 bf16x4_t __attribute__((ext_vector_type(4)));
+    const int col0 = wn * 64 + 4 * (lane >> 4), i0 = nt * kTileN + col0;
+    auto each = [&](auto put) {
 #pragma unroll
-    for (int m = 0; m < HB; ++m) {
-        const int tr = (wm * HB + m) * 16 + (lane & 15);
-        if (tr >= rows) continue;
+        for (int m = 0; m < HB; ++m)
 #pragma unroll
-        for (int nb = 0; nb < 4; ++nb) {
-            const int col = wn * 64 + nb * 16 + c4, i = nt * kTileN + col;
-            floatx4_t s = acc[m][nb];
-            if (part) {
-                *reinterpret_cast<floatx4_t *>(part + (size_t)tr * kTileN + col) = s;
-            } else if (i < p.o) {
-                typedef __bf16 bf16x4_t __attribute__((ext_vector_type(4)));
-                const size_t t = row0 + tr;
-                if (p.bf16) {
-                    if (p.y_in) {
-                        const bf16x4_t b = *reinterpret_cast<const bf16x4_t *>(static_cast<const __bf16 *>(p.y_in) + t * p.ldyin + i);
-                        for (int c = 0; c < 4; ++c) s[c] += static_cast<float>(b[c]);
-                    }
-                    bf16x4_t o;
-                    for (int c = 0; c < 4; ++c) o[c] = static_cast<__bf16>(s[c]);
-                    *reinterpret_cast<bf16x4_t *>(static_cast<__bf16 *>(p.y) + t * p.ldy + i) = o;
-                } else {
-                    if (p.y_in) s += *reinterpret_cast<const floatx4_t *>(static_cast<const float *>(p.y_in) + t * p.ldyin + i);
-                    *reinterpret_cast<floatx4_t *>(static_cast<float *>(p.y) + t * p.ldy + i) = s;
-                }
+            for (int nb = 0; nb < 4; ++nb) {
+                const int tr = (wm * HB + m) * 16 + (lane & 15);
+                if (tr < rows && i0 + nb * 16 < p.o) put(tr, nb, acc[m][nb]);
             }
+    };
+    if (part) {
+#pragma unroll
+        for (int m = 0; m < HB; ++m) {
+            const int tr = (wm * HB + m) * 16 + (lane & 15);
+            if (tr >= rows) continue;
+#pragma unroll
+            for (int nb = 0; nb < 4; ++nb) *reinterpret_cast<floatx4_t *>(part + (size_t)tr * kTileN + col0 + nb * 16) = acc[m][nb];
         }
+        return;
+    }
+    if (p.y_in) {   // the loads of a block of tokens together: y may be y_in, so the compiler would wait for each
+#pragma unroll
+        for (int m = 0; m < HB; ++m) {
+            const size_t at = (row0 + min((wm * HB + m) * 16 + (lane & 15), rows - 1)) * p.ldyin;
+            if (p.bf16) {
+                bf16x4_t in[4];
+#pragma unroll
+                for (int nb = 0; nb < 4; ++nb)
+                    in[nb] = *reinterpret_cast<const bf16x4_t *>(static_cast<const __bf16 *>(p.y_in) + at + min(i0 + nb * 16, p.o - 4));
+#pragma unroll
+                for (int nb = 0; nb < 4; ++nb)
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) acc[m][nb][c] += static_cast<float>(in[nb][c]);
+            } else {
+#pragma unroll
+                for (int nb = 0; nb < 4; ++nb)
+                    acc[m][nb] += *reinterpret_cast<const floatx4_t *>(static_cast<const float *>(p.y_in) + at + min(i0 + nb * 16, p.o - 4));
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    }
+    if (p.bf16) {
+        each([&](int tr, int nb, const floatx4_t v) {
+            bf16x4_t o;
+#pragma unroll
+            for (int c = 0; c < 4; ++c) o[c] = static_cast<__bf16>(v[c]);
+            *reinterpret_cast<bf16x4_t *>(static_cast<__bf16 *>(p.y) + (size_t)(row0 + tr) * p.ldy + i0 + nb * 16) = o;
+        });
+    } else {
+        each([&](int tr, int nb, const floatx4_t v) {
+            *reinterpret_cast<floatx4_t *>(static_cast<float *>(p.y) + (size_t)(row0 + tr) * p.ldy + i0 + nb * 16) = v;
+        });
     }
 }
 
