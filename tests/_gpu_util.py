@@ -24,6 +24,41 @@ def torch_cuda():
     return torch
 
 
+_side = []
+
+
+def side_streams(torch):
+    """Four streams beside the default one, the same in every test that asks.
+
+    torch hands out a pool of 32 streams in turn, and HIP runs them on four hardware queues, so
+    whether a stream that a test holds back also holds back another depends on how many were taken
+    before. One whole turn is taken here, and one stream used per queue: what tests of other
+    files get does not depend on the tests that ran before them."""
+    if not _side:
+        turn = [torch.cuda.Stream() for _ in range(32)]
+        _side.extend(turn[:4])
+        for s in _side:
+            with torch.cuda.stream(s):
+                torch.zeros(1, device="cuda")
+        torch.cuda.synchronize()
+    return _side
+
+
+def capture(torch, call):
+    """A graph of `call`, which has run on the capturing stream once before."""
+    side = side_streams(torch)[0]
+    graph = torch.cuda.CUDAGraph()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        call()
+        side.synchronize()
+        graph.capture_begin()
+        call()
+        graph.capture_end()
+    torch.cuda.current_stream().wait_stream(side)
+    return graph
+
+
 def rel_err(got, ref):
     ref = np.asarray(ref, dtype=np.float64)
     got = np.asarray(got, dtype=np.float64)

@@ -10,7 +10,7 @@ long batches have two parts (2^-17 relative), and y is rounded once, by at most 
 import numpy as np
 import pytest
 
-from _gpu_util import say, torch_cuda
+from _gpu_util import capture, say, side_streams, torch_cuda
 
 pytestmark = pytest.mark.gpu
 
@@ -201,14 +201,7 @@ def test_captured_and_replayed(T):
     say("adapter graph", T)
     c = Case(torch, 3, T, 1032, 1288, 16, 6, "bfloat16", "each")
     y, ws = torch.empty((T, c.o), dtype=c.dtype, device="cuda"), c.workspace()
-    side = torch.cuda.Stream()
-    side.wait_stream(torch.cuda.current_stream())
-    with torch.cuda.stream(side):
-        c.call(y, ws)
-    torch.cuda.current_stream().wait_stream(side)
-    graph = torch.cuda.CUDAGraph()
-    with torch.cuda.graph(graph):
-        c.call(y, ws)
+    graph = capture(torch, lambda: c.call(y, ws))
     for i in range(4):
         c.x.copy_(torch.randn(c.x.shape, device="cuda", generator=torch.Generator("cuda").manual_seed(i)).to(c.dtype))
         c.ids.copy_((c.ids + 2) % 7 - 1)
@@ -223,7 +216,7 @@ def test_two_streams_at_once(T):
     say("adapter two streams", T)
     cases = [Case(torch, 5 + i, T, 2056, 1288 + 512 * i, 16, 6, "bfloat16", "each") for i in range(2)]
     alone = [c.run() for c in cases]
-    streams = [torch.cuda.Stream() for _ in range(2)]
+    streams = side_streams(torch)[:2]
     ws = [c.workspace() for c in cases]
     ys = [[torch.empty((T, c.o), dtype=c.dtype, device="cuda") for _ in range(5)] for c in cases]
     torch.cuda.synchronize()

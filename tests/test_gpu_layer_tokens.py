@@ -12,7 +12,7 @@ to 2^-17 (two parts, the second rounded: 2^-8 of 2^-8, halved), and rounds y onc
 import numpy as np
 import pytest
 
-from _gpu_util import say, torch_cuda
+from _gpu_util import capture, say, side_streams, torch_cuda
 
 pytestmark = pytest.mark.gpu
 
@@ -296,14 +296,7 @@ def test_captured_and_replayed(T, n):
     layer = Layer(torch, 15, 512, 520, n, 2, 136)
     x = states(torch, 8, T, 512, torch.float32)
     y, ws = torch.empty_like(x), layer.workspace(T)
-    side = torch.cuda.Stream()
-    side.wait_stream(torch.cuda.current_stream())
-    with torch.cuda.stream(side):
-        layer.call(x, y, ws)
-    torch.cuda.current_stream().wait_stream(side)
-    graph = torch.cuda.CUDAGraph()
-    with torch.cuda.graph(graph):
-        layer.call(x, y, ws)
+    graph = capture(torch, lambda: layer.call(x, y, ws))
     for i in range(4):
         x.copy_(states(torch, 20 + i, T, 512, torch.float32))
         graph.replay()
@@ -319,7 +312,7 @@ def test_two_streams_at_once():
     layers = [Layer(torch, 30 + i, 1024, 1024 + 8 * i, 8, 2) for i in range(2)]
     x = states(torch, 9, 8, 1024, torch.float32)
     alone = [l.run(x)[0] for l in layers]
-    streams = [torch.cuda.Stream() for _ in range(2)]
+    streams = side_streams(torch)[:2]
     ws = [l.workspace(8) for l in layers]
     ys = [[torch.empty_like(x) for _ in range(5)] for _ in range(2)]
     torch.cuda.synchronize()
