@@ -206,13 +206,13 @@ constexpr int kKeptSums = 4096;   // 16 KiB: 8 tokens of 32 items
 
 // W x and B v for up to 16 tokens. A work group takes an equal, contiguous share of the (group, 16
 // rows) items; the adapters' part belongs to group 0. E: stages of B per item.
-template <int S, int E, int NB>
+template <int S, int E, int NB, bool NT>
 __global__ __launch_bounds__(kThreads) void k_adapter_rows(AdapterParams p)
 {
     constexpr bool STK = NB == 3;
     constexpr int AB = STK ? 1 : NB;
     constexpr int kRankPitch = MOE_ADAPTER_MAX_RANK + 8;   // values; the pad spreads the tokens over the banks
-    using Stream_t = Stream<S + E, RowsSrc<S>, RowsAndB<S>>;
+    using Stream_t = Stream<S + E, RowsSrc<S>, RowsAndB<S>, NT>;
     __shared__ __align__(1024) uint8_t lds[kWaves * Stream_t::kBytes];
     __shared__ __align__(16) Sums<AB> sums;
     __shared__ __align__(16) uint16_t v[3 * kStreamTokens * kRankPitch];
@@ -1035,8 +1035,10 @@ hipError_t launch_rows(const AdapterParams &p, hipStream_t s)
 {
     const dim3 grid((unsigned)std::min<int64_t>(device_cu_count(), (int64_t)p.groups * ceil_div(p.o, kRows)));
     // stages of B: a wave has one adapter per 8 tokens, and a stage per 64 ranks
-    if (ceil_div(p.T, kWaves) * ceil_div(p.r, kChunk) <= 2) hipLaunchKernelGGL((k_adapter_rows<S, 2, NB>), grid, dim3(kThreads), 0, s, p);
-    else hipLaunchKernelGGL((k_adapter_rows<S, 4, NB>), grid, dim3(kThreads), 0, s, p);
+    const bool two = ceil_div(p.T, kWaves) * ceil_div(p.r, kChunk) <= 2, nt = whole_lines(p.d * 2);
+    const auto kernel = two ? (nt ? k_adapter_rows<S, 2, NB, true> : k_adapter_rows<S, 2, NB, false>)
+                            : (nt ? k_adapter_rows<S, 4, NB, true> : k_adapter_rows<S, 4, NB, false>);
+    hipLaunchKernelGGL(kernel, grid, dim3(kThreads), 0, s, p);
     return hipGetLastError();
 }
 

@@ -288,12 +288,12 @@ constexpr int most_tokens(int S) { return S == 1 ? kMaxTok : MOE_LAYER_MAX_VALUE
 // (11 tokens through experts of 1048 x 1816, three chunks a block: 118 us with one, 109 with two).
 constexpr int gate_up_blocks(int S, int AB) { return S <= 4 && AB == 1 ? 2 : 1; }
 
-template <int S, int NB>
+template <int S, int NB, bool NT>
 __global__ __launch_bounds__(kThreads) void k_layer_gate_up(LayerParams p)
 {
     constexpr bool STK = NB == 3;
     constexpr int AB = STK ? 1 : NB, R = gate_up_blocks(S, AB);
-    using Stream_t = Stream<S, GateUpSrc<R>>;
+    using Stream_t = Stream<S, GateUpSrc<R>, Rows, NT>;
     using Sums_t = Sums<R * AB>;
     __shared__ __align__(1024) uint8_t lds[kWaves * Stream_t::kBytes];
     constexpr size_t kLogits = sizeof(double) * most_tokens(S) * (MOE_MAX_EXPERTS + MOE_MAX_TOPK_INTERNAL);
@@ -447,11 +447,11 @@ constexpr int kKeptSums = 4096;   // 16 KiB: 8 tokens of 32 items
 // Down: the sums of group g (eight units of hidden columns) for 16 rows of W2 and all tokens. A
 // work group takes an equal, contiguous share of the (group, row block) items. one: there is one
 // group, whose sums are the layer's output.
-template <int S, int NB, bool STK>
+template <int S, int NB, bool STK, bool NT>
 __global__ __launch_bounds__(kThreads) void k_layer_down(LayerParams p, bool one)
 {
     constexpr int AB = STK ? 1 : NB;
-    using Stream_t = Stream<S, DownSrc>;
+    using Stream_t = Stream<S, DownSrc, Rows, NT>;
     __shared__ __align__(1024) uint8_t lds[kWaves * Stream_t::kBytes];
     __shared__ __align__(16) Sums<AB> sums;
     __shared__ Jobs J;
@@ -560,7 +560,8 @@ LayerPlan plan_layer(int T, int d, int f, int n, int k, int fs, bool bf16)
 template <int S, int NB>
 hipError_t launch_gate_up(const LayerParams &p, hipStream_t s)
 {
-    hipLaunchKernelGGL((k_layer_gate_up<S, NB>), dim3(device_cu_count()), dim3(kThreads), 0, s, p);
+    const auto kernel = whole_lines(p.d * 2) ? k_layer_gate_up<S, NB, true> : k_layer_gate_up<S, NB, false>;
+    hipLaunchKernelGGL(kernel, dim3(device_cu_count()), dim3(kThreads), 0, s, p);
     return hipGetLastError();
 }
 
@@ -569,7 +570,8 @@ hipError_t launch_down(const LayerParams &p, int groups, hipStream_t s)
 {
     const int rbs = ceil_div(p.d, kRows);
     const dim3 grid((unsigned)std::min<int64_t>(device_cu_count(), (int64_t)groups * rbs));
-    hipLaunchKernelGGL((k_layer_down<S, NB, STK>), grid, dim3(kThreads), 0, s, p, groups == 1);
+    const auto kernel = whole_lines(p.f * 2) ? k_layer_down<S, NB, STK, true> : k_layer_down<S, NB, STK, false>;
+    hipLaunchKernelGGL(kernel, grid, dim3(kThreads), 0, s, p, groups == 1);
     return hipGetLastError();
 }
 

@@ -13,9 +13,7 @@
 // Reading 2 GiB this way (rows of 8 KiB, nothing multiplied) runs at 6.80 TB/s, and at 6.94
 // where 8 KiB are read of each 28 KiB row; loading the same fragments into registers (16
 // rows by 64 bytes per instruction) gives 6.0 and 5.2, one contiguous KiB per instruction
-// 7.0, and loads that keep the lines in the caches 6.1 (a Mixtral-shaped layer for one token 121 us
-// and 136 so; only rows that begin inside a 128-byte line, whose lines are read again for the next
-// chunk, would gain: 11 tokens through experts of 1048 x 1816 107 and 104).
+// 7.0, and loads that keep the lines in the caches 6.1.
 //
 // fp32 activations are cut into three bf16 parts of 8 bits each, v = hi + mid + lo exactly,
 // which take three columns of the B operand: the products with bf16 weights are then exact
@@ -141,6 +139,13 @@ __device__ __forceinline__ Place place_of(const Rows &r, int s, const uint8_t *h
             real ? (uint32_t)(r.lane_row + min((r.c0 + s) * (kChunk * 2) + lane_piece(), r.bytes - 16)) : 0u};
 }
 
+// Rows of `bytes` bytes end with a 128-byte line, so that a line is read for one chunk only and need
+// not be kept: a Mixtral-shaped layer for one token takes 122 us with nontemporal loads, 136 with
+// plain ones. Other rows' lines are read again for the next chunk: the layer with rows of 4104 and 14344
+// values 157 and 142 us, 8 tokens with adapters on 4104 x 14344 44.5 and 42, 11 tokens through
+// experts of 1048 x 1816 106 and 103. (A choice in the loop costs 1.5 %, so there are two of each kernel.)
+__host__ __device__ constexpr bool whole_lines(int bytes) { return bytes % 128 == 0; }
+
 // Stages of a ring for items of S stages: at most 4 (64 KiB on their way per work group hide the
 // memory's latency: 470 MB read in 71.5 us with 4 stages, 72.0 with 8; the layer's cases took the
 // same time, within 1 %, with 3, 4 and 5), and a whole number of items, or less than one.
@@ -153,7 +158,9 @@ __host__ __device__ constexpr int ring_stages(int S) { return S >= 4 ? 4 : S * (
 // is two loads, always, so that the wait is a constant: stages that an item does not have, and
 // those past the last item, read 16 bytes at `hot` over and over, and are not multiplied.
 // Src: next() gives the wave's next item, whose stages place_of() finds (past the last: none real).
-template <int S, class Src, class Item = Rows>
+// NT: the loads do not keep their lines in the caches, which is better for rows of whole lines only
+// (whole_lines()).
+template <int S, class Src, class Item = Rows, bool NT = true>
 struct Stream {
     static constexpr int RS = ring_stages(S);
     static constexpr bool kWhole = RS % S == 0;   // the ring holds whole items: RS / S of them
@@ -167,8 +174,8 @@ struct Stream {
     {
         const Place p = place_of(r, s, hot);
         uint8_t *to = lds + at * kStageBytes;
-        __builtin_amdgcn_global_load_lds((global_cvoid *)(p.b0 + p.o), (lds_void *)to, 16, 0, 2);   // 2: nontemporal
-        __builtin_amdgcn_global_load_lds((global_cvoid *)(p.b1 + p.o), (lds_void *)(to + kStageBytes / 2), 16, 0, 2);
+        __builtin_amdgcn_global_load_lds((global_cvoid *)(p.b0 + p.o), (lds_void *)to, 16, 0, NT ? 2 : 0);   // 2: nontemporal
+        __builtin_amdgcn_global_load_lds((global_cvoid *)(p.b1 + p.o), (lds_void *)(to + kStageBytes / 2), 16, 0, NT ? 2 : 0);
     }
     __device__ __forceinline__ void start(Src &src, uint8_t *ring, const uint8_t *hot_bytes)
     {
